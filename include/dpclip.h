@@ -29,9 +29,10 @@
  *   - All tensors are dense row-major.  A, Xhat: [B, T, d_in|d];  G: [B, T, d_out|d];  ids: int32 [B, T];
  *     weight-shaped sums: [d_in, d_out];  embedding sums: [V, d].  sqnorms, sums, params, m, v: fp32.
  *   - dtype selects the element type of A / Xhat / G: DP_F32 (4-byte aligned) or DP_BF16 (16-byte aligned
- *     pointers and d_in, d_out, d multiples of 8).  Accumulation is always fp32.
+ *     pointers and d_in, d_out, d multiples of 8, except where a call says that it needs an element's alignment only).
+ *     Accumulation is always fp32.
  *   - Calls are asynchronous on the context's stream and return argument and launch errors at once.
- *     Errors found on the device (a token id outside [0, V)) are returned by the next dp_sync.
+ *     Errors found on the device (a token id outside [0, V), a position outside its table) are returned by the next dp_sync.
  *   - Results are deterministic: the same call sequence on the same inputs gives the same bits.
  *   - The step's entry points (norms, clip factors, clip-weighted sums, the update, dp_zero_f32) only launch kernels
  *     on the context's stream: no allocation, no memory-set or copy command, no wait for the device.  A caller may
@@ -64,7 +65,7 @@ typedef enum {
     DP_ERR_ALIGN = -4,     /* pointer alignment */
     DP_ERR_VALUE = -5,     /* C <= 0, sigma < 0, batch_size == 0, step == 0, beta outside [0,1), eps < 0 ...; from dp_sync: a
                               per-example squared norm that pass 2 read was NaN or had overflowed fp32 */
-    DP_ERR_INDEX = -6,     /* a token id outside [0, V) was met on the device (reported by dp_sync) */
+    DP_ERR_INDEX = -6,     /* a token id outside [0, V), or a position outside its table, was met on the device (reported by dp_sync) */
     DP_ERR_WORKSPACE = -7, /* the context's workspace is too small for this call */
     DP_ERR_HIP = -8        /* a HIP runtime call failed; dp_last_error has the text */
 } dp_status;
@@ -76,7 +77,7 @@ dp_status dp_create(dp_ctx** out, void* hip_stream, size_t workspace_bytes);
 /* Synchronise the stream, then free the workspace and the context. */
 dp_status dp_destroy(dp_ctx* ctx);
 /* hipStreamSynchronize, then fetch-and-clear the device error word: DP_OK, DP_ERR_INDEX (a token id outside
- * [0, V)), DP_ERR_VALUE (a non-finite squared norm met by pass 2; DP_ERR_INDEX wins if both occurred) or DP_ERR_HIP. */
+ * [0, V), a position outside its table), DP_ERR_VALUE (a non-finite squared norm met by pass 2; DP_ERR_INDEX wins if both occurred) or DP_ERR_HIP. */
 dp_status dp_sync(dp_ctx* ctx);
 const char* dp_status_str(dp_status s);
 /* Text of the last error of this context; static storage inside the context. */
@@ -232,6 +233,83 @@ dp_status dp_clip_accumulate_tied_embedding(dp_ctx* ctx, const int32_t* ids, con
 
 /* The clip factors themselves (pass 2 computes them internally; exposed for checks): c[i], i < B. */
 dp_status dp_clip_factors(dp_ctx* ctx, const float* sqnorms, int B, float C, float* c);
+
+/* ---------------------------------------------------------------------------------------------------
+ * Gradients that the caller holds: n_layers tensors X[l] of B gradients each, [B, counts[l]], dense, of one dtype, every gradient of a
+ * tensor on its own (B examples of a layer that has no form above, as a vectorised backward leaves them; the per-example gradients that
+ * dp_relative_bias_grads and dp_qk_norm_grads write) or, with B = 1, the whole gradient of one unit that is clipped as such (a user, a
+ * micro-batch).  The norms add to those of the other calls of pass 1.  X and counts are HOST arrays, read during the call only; pointers
+ * need the alignment of an element only, counts any value; tensors of no elements are passed over, their pointer is not looked at.
+ * Tensors of different types go into calls of their own.  Up to 120 tensors share a launch.
+ * ------------------------------------------------------------------------------------------------- */
+
+/* sqnorms[i] += sum_l sum_k X[l][i, k]^2.  The norms of a tensor's pieces pass through the workspace (a float per unit for every tensor,
+ * more for long ones); fewer tensors share a launch where they do not fit, DP_ERR_WORKSPACE if those of one tensor do not. */
+dp_status dp_sqnorms_grads(dp_ctx* ctx, int n_layers, const void* const* X, const uint64_t* counts, dp_dtype dtype, int B, float* sqnorms);
+
+/* sums[l][k] += sum_i c_i X[l][i, k] (fp32).  Tensors whose sums overlap add to them launch after launch; no sum overlaps an X. */
+dp_status dp_clip_accumulate_grads(dp_ctx* ctx, int n_layers, const void* const* X, const uint64_t* counts, dp_dtype dtype, int B, float C,
+                                   const float* sqnorms, float* const* sums);
+
+/* Y[l][i, k] = c_i X[l][i, k], of X's dtype, rounded once: every unit's gradient clipped to norm C.  Y[l] is X[l] (clipped in place;
+ * units whose norm is within C are then not touched) or overlaps no X and no other Y. */
+dp_status dp_clip_grads(dp_ctx* ctx, int n_layers, const void* const* X, const uint64_t* counts, dp_dtype dtype, int B, float C,
+                        const float* sqnorms, void* const* Y);
+
+/* ---------------------------------------------------------------------------------------------------
+ * A relative position bias learned by buckets of distance: a table [n or 2 n, H] (one row per bucket), added to the attention scores of
+ * H heads, often by all layers of a stack.  The Tq queries are the last of the Tk positions (Tq == Tk: self-attention; Tq == 1: one new
+ * token): query q stands at p = Tk - Tq + q, and a key k at distance k - p.  Distances in front of the query (k <= p) have the buckets
+ * 0 .. n - 1, bucket j the distances starts[j] <= p - k < starts[j + 1], the last one all from starts[n - 1] on.  Keys behind it (k > p)
+ * have the buckets n .. 2 n - 1 by the same starts if bidirectional, else the bucket of distance 0.  starts is a HOST array, read during
+ * the call only: starts[0] == 0, none below the one before it (equal ones: a bucket without distances), none above 2^30; n in [1, 128].
+ * ------------------------------------------------------------------------------------------------- */
+
+/* Host-only, pure: the customary starts of n buckets.  The first n / 2 are one distance each, 0 .. n/2 - 1; the others grow in equal steps
+ * of the logarithm up to max_distance: starts[n/2 + j] is the first distance d with (d / (n/2))^(n - n/2) >= (max_distance / (n/2))^j,
+ * decided in whole numbers.  DP_ERR_VALUE unless 2 <= n <= 128 and n/2 < max_distance <= 2^30. */
+dp_status dp_relative_buckets(int n, int max_distance, int32_t* starts);
+
+/* bias[h, q, k] = table[bucket(k - p), h] for all pairs, [H, Tq, Tk] of `dtype` (rounded once), element alignment; table fp32. */
+dp_status dp_relative_bias(dp_ctx* ctx, const float* table, int n, const int32_t* starts, int bidirectional, int H, int Tq, int Tk,
+                           dp_dtype dtype, void* bias);
+
+/* Every example's gradient of the table, from the gradients of the attention scores of the n_layers layers that use it, dS[l] [B, H, Tq, Tk]
+ * of `dtype` (element alignment, any Tk):
+ *     grads[i, b, h] = sum_l sum_{q, k: bucket(k - p) = b} dS[l][i, h, q, k]        [B, n or 2 n, H], fp32, overwritten.
+ * lengths: int32 [B] on the device, or NULL: only queries and keys at positions below lengths[i] count (clamped to [0, Tk]); causal != 0:
+ * only keys k <= p.  What lies elsewhere is not used, whatever it holds (NaN of a row that its mask leaves empty).  n_layers == 0 writes
+ * zeros.  grads is what dp_sqnorms_grads and dp_clip_accumulate_grads take.  Sums in fp32.  DP_ERR_SHAPE if Tq > Tk or Tq + Tk > 32768.
+ * With few examples and heads the parts of a plane pass through the workspace.  dS is a HOST array, read during the call only. */
+dp_status dp_relative_bias_grads(dp_ctx* ctx, int n_layers, const void* const* dS, dp_dtype dtype, const int32_t* lengths, int causal, int n,
+                                 const int32_t* starts, int bidirectional, int B, int H, int Tq, int Tk, float* grads);
+
+/* ---------------------------------------------------------------------------------------------------
+ * Norms of queries and keys: every head's D numbers x of a token become y = Rot_p(g * x r), r = 1 / sqrt(mean_j x_j^2 + eps), with one gain
+ * g [D] (fp32) for the query heads and one for the key heads, and Rot_p the rotation of the first R numbers by the token's position p:
+ *     (y_a, y_b) = (z_a cos[p, j] - z_b sin[p, j], z_b cos[p, j] + z_a sin[p, j]),  j < R / 2,
+ * a = 2 j, b = 2 j + 1 if interleaved, else a = j, b = R / 2 + j.  cos, sin: fp32 [n_pos, R / 2] on the device (not read if R == 0);
+ * positions: int32 [B, T] on the device, or NULL: p is the token's place in its example.  A position outside [0, n_pos) is reported by
+ * dp_sync as DP_ERR_INDEX; its token's outputs are zero and it adds nothing to the gradients.
+ *   q, k: [B, T, Hq, D] and [B, T, Hk, D] of `dtype`, a token's heads next to each other, tokens ldq / ldk numbers apart (at least Hq D / Hk D;
+ *   more where they are parts of a fused projection's output).  Either may have no heads (its pointers are not looked at).  Element alignment.
+ *   D in [8, 512] and R in [0, D], both multiples of 8; eps > 0.  No output overlaps an input (DP_ERR_VALUE).  Arithmetic in fp32.
+ * ------------------------------------------------------------------------------------------------- */
+
+/* yq [B, T, Hq, D], yk [B, T, Hk, D], dense. */
+dp_status dp_qk_norm(dp_ctx* ctx, const void* q, const void* k, dp_dtype dtype, int64_t ldq, int64_t ldk, const float* gain_q,
+                     const float* gain_k, const float* cos, const float* sin, int n_pos, const int32_t* positions, int interleaved, int B,
+                     int T, int Hq, int Hk, int D, int R, float eps, void* yq, void* yk);
+
+/* The backward, from dyq, dyk (dense, as yq, yk): with u = Rot_p^T dy, xhat = x r,
+ *     grads[i, 0, :] = sum over example i's tokens and query heads of u xhat, grads[i, 1, :] over its key heads   ([B, 2, D] fp32, overwritten)
+ *     dx = r (g u - xhat mean_j(g_j u_j xhat_j))     written to dq, dk, laid out as q, k (same ldq, ldk); both NULL: not wanted.
+ * grads is what dp_sqnorms_grads and dp_clip_accumulate_grads take, as one tensor of 2 D numbers.  T == 0 writes zeros.  The parts of
+ * long examples pass through the workspace. */
+dp_status dp_qk_norm_grads(dp_ctx* ctx, const void* q, const void* k, dp_dtype dtype, int64_t ldq, int64_t ldk, const float* gain_q,
+                           const float* gain_k, const float* cos, const float* sin, int n_pos, const int32_t* positions, int interleaved,
+                           int B, int T, int Hq, int Hk, int D, int R, float eps, const void* dyq, const void* dyk, float* grads, void* dq,
+                           void* dk);
 
 /* ---------------------------------------------------------------------------------------------------
  * Update (Algorithm 1, g_t line to theta_t line) over the slice [elem_offset, elem_offset + n) of the

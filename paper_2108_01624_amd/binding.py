@@ -5,7 +5,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import c_char_p, c_float, c_int, c_size_t, c_uint64, c_void_p
+from ctypes import c_char_p, c_float, c_int, c_int64, c_size_t, c_uint64, c_void_p
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libdpclip.so")
 _NATIVE_PATH = os.path.join(os.path.dirname(_LIB_PATH), "_native.so")
@@ -52,6 +52,17 @@ SIGNATURES = {
                                   c_void_p],
     "dp_clip_accumulate_tied_embedding": [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_int, c_int, c_int, c_int,
                                           c_int, c_float, c_void_p, c_void_p],
+    "dp_sqnorms_grads": [c_void_p, c_int, c_void_p, ctypes.POINTER(c_uint64), c_int, c_int, c_void_p],
+    "dp_clip_accumulate_grads": [c_void_p, c_int, c_void_p, ctypes.POINTER(c_uint64), c_int, c_int, c_float, c_void_p, c_void_p],
+    "dp_clip_grads": [c_void_p, c_int, c_void_p, ctypes.POINTER(c_uint64), c_int, c_int, c_float, c_void_p, c_void_p],
+    "dp_relative_buckets": [c_int, c_int, ctypes.POINTER(ctypes.c_int32)],
+    "dp_relative_bias": [c_void_p, c_void_p, c_int, ctypes.POINTER(ctypes.c_int32), c_int, c_int, c_int, c_int, c_int, c_void_p],
+    "dp_relative_bias_grads": [c_void_p, c_int, c_void_p, c_int, c_void_p, c_int, c_int, ctypes.POINTER(ctypes.c_int32), c_int, c_int, c_int,
+                               c_int, c_int, c_void_p],
+    "dp_qk_norm": [c_void_p, c_void_p, c_void_p, c_int, c_int64, c_int64, c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_void_p, c_int, c_int,
+                   c_int, c_int, c_int, c_int, c_int, c_float, c_void_p, c_void_p],
+    "dp_qk_norm_grads": [c_void_p, c_void_p, c_void_p, c_int, c_int64, c_int64, c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_void_p, c_int,
+                         c_int, c_int, c_int, c_int, c_int, c_int, c_float, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p],
     "dp_noise_adamw": [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_uint64, c_uint64, c_float, c_float, c_uint64,
                        c_uint64, c_uint64, c_float, c_float, c_float, c_float, c_float, c_int],
     "dp_noise_adamw_snr": [c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_uint64, c_uint64, c_float, c_float, c_uint64,
@@ -396,6 +407,186 @@ def dp_clip_accumulate_tied_embedding(ctx, ids, dY, H, dL, C, sqnorms, sum_E):
     st = load_library().dp_clip_accumulate_tied_embedding(ctx, _i32(ids), _ptr(dY), _ptr(H), _ptr(dL), _dtype_of(dY), B, T, M,
                                                           d, V, float(C), _f32(sqnorms), _f32(sum_E))
     _check(ctx, st, "dp_clip_accumulate_tied_embedding")
+
+
+# ---- gradients that the caller holds, and the parameters that write such gradients ----------------------------------------------
+# These calls read tensors of any size and layout of heads, so their functions check what an address does not say: that a tensor is dense, where
+# it lies, and that its size is the one the call will assume.
+def _where(*tensors):
+    """Refuses tensors that are not all on one device, or on the CPU beside a GPU."""
+    import torch
+
+    dev = None
+    for t in tensors:
+        if t is None:
+            continue
+        if dev is None:
+            dev = t.device
+            if dev.type != "cuda" and torch.cuda.is_available():
+                raise ValueError(f"tensors in device memory expected, got one on {dev}")
+        elif t.device != dev:
+            raise ValueError(f"tensors on {dev} and {t.device} in one call")
+
+
+def _dense(what, t):
+    if not t.is_contiguous():
+        raise ValueError(f"{what}: a dense (contiguous) tensor expected")
+    return t
+
+
+def _held(Xs, sqnorms, outs, what, whole):
+    """(addresses, elements of a unit, dtype code, units, addresses of the outputs) of tensors [units, ...], one per norm; `whole`: outputs
+    have a gradient per unit too, of the same type.  One norm: the whole of every tensor is the gradient of the one unit."""
+    B = _dense("sqnorms", sqnorms).numel()
+    if sqnorms.dim() > 1:
+        raise ValueError("sqnorms: one number per unit")
+    if outs is not None and len(outs) != len(Xs):
+        raise ValueError(f"{len(outs)} {what} for {len(Xs)} tensors")
+    _where(sqnorms, *Xs, *(outs or ()))
+    n = len(Xs)
+    counts, ptrs, out_ptrs = [], [], []
+    dt = Xs[0].dtype if n else sqnorms.dtype
+    for k, x in enumerate(Xs):
+        if x.dtype != dt:
+            raise ValueError("all tensors of a call must share one dtype")
+        if B != 1 and (x.dim() == 0 or x.shape[0] != B):
+            raise ValueError(f"tensor {k} of shape {tuple(x.shape)}: gradients of {B} units expected")
+        counts.append(x.numel() // B if B else 0)
+        ptrs.append(_dense(f"tensor {k}", x).data_ptr())
+        if outs is not None:
+            y = _dense(f"{what} {k}", outs[k])
+            if y.numel() != (x.numel() if whole else counts[-1]):
+                raise ValueError(f"{what} {k} holds {y.numel()} numbers, {x.numel() if whole else counts[-1]} expected")
+            if whole and y.dtype != dt:
+                raise ValueError(f"{what} {k}: {dt} expected, got {y.dtype}")
+            out_ptrs.append(y.data_ptr() if whole else _f32(y))
+    return (c_void_p * n)(*ptrs), (c_uint64 * n)(*counts), _dtype_code(dt), B, (c_void_p * n)(*out_ptrs) if outs is not None else None
+
+
+def dp_sqnorms_grads(ctx, Xs, sqnorms):
+    """Xs: tensors [B, ...], the gradients of B units each, B the size of sqnorms; B == 1: tensors of any shape, all of one unit."""
+    ptrs, counts, dt, B, _ = _held(Xs, sqnorms, None, "", False)
+    _check(ctx, load_library().dp_sqnorms_grads(ctx, len(Xs), ptrs, counts, dt, B, _f32(sqnorms)), "dp_sqnorms_grads")
+
+
+def dp_clip_accumulate_grads(ctx, Xs, C, sqnorms, sums):
+    """sums: one float32 tensor per tensor of Xs, of the size of one unit's gradient."""
+    ptrs, counts, dt, B, out = _held(Xs, sqnorms, sums, "sums", False)
+    st = load_library().dp_clip_accumulate_grads(ctx, len(Xs), ptrs, counts, dt, B, float(C), _f32(sqnorms), out)
+    _check(ctx, st, "dp_clip_accumulate_grads")
+
+
+def dp_clip_grads(ctx, Xs, C, sqnorms, Ys):
+    """Ys: one tensor per tensor of Xs, of its type and size; the same one: clipped in place."""
+    ptrs, counts, dt, B, out = _held(Xs, sqnorms, Ys, "outputs", True)
+    _check(ctx, load_library().dp_clip_grads(ctx, len(Xs), ptrs, counts, dt, B, float(C), _f32(sqnorms), out), "dp_clip_grads")
+
+
+def dp_relative_buckets(n, max_distance) -> list:
+    """The first distances of n buckets of a side, half of them one distance each, the others in equal steps of the logarithm (host only)."""
+    if n > 128:
+        raise DpError(-5, "dp_relative_buckets", "at most 128 buckets of a side")
+    buf = (ctypes.c_int32 * max(n, 1))()
+    st = load_library().dp_relative_buckets(n, max_distance, buf)
+    if st != DP_OK:
+        raise DpError(st, "dp_relative_buckets")
+    return list(buf)
+
+
+def dp_relative_bias(ctx, table, starts, bidirectional, bias):
+    """table [buckets, H] (float32), buckets = len(starts), twice that if bidirectional; bias [H, Tq, Tk], overwritten."""
+    n, (H, Tq, Tk) = len(starts), bias.shape
+    if tuple(table.shape) != (n * (2 if bidirectional else 1), H):
+        raise ValueError(f"table of shape {tuple(table.shape)}: [{n * (2 if bidirectional else 1)}, {H}] expected")
+    _where(table, bias)
+    st = load_library().dp_relative_bias(ctx, _f32(_dense("table", table)), n, (ctypes.c_int32 * n)(*starts), int(bool(bidirectional)), H, Tq, Tk,
+                                         _dtype_of(bias), _dense("bias", bias).data_ptr())
+    _check(ctx, st, "dp_relative_bias")
+
+
+def dp_relative_bias_grads(ctx, dSs, starts, bidirectional, grads, *, lengths=None, causal=False):
+    """dSs: one tensor [B, H, Tq, Tk] per layer that uses the table (gradients of the attention scores); grads [B, buckets, H], overwritten;
+    lengths: int32 [B] or None."""
+    n, (B, H, Tq, Tk), dt = len(starts), dSs[0].shape, dSs[0].dtype
+    for x in dSs:
+        if tuple(x.shape) != (B, H, Tq, Tk) or x.dtype != dt:
+            raise ValueError("all layers of a call must share one shape and dtype")
+        _dense("dS", x)
+    if tuple(grads.shape) != (B, n * (2 if bidirectional else 1), H):
+        raise ValueError(f"grads of shape {tuple(grads.shape)}: {(B, n * (2 if bidirectional else 1), H)} expected")
+    if lengths is not None and tuple(lengths.shape) != (B,):
+        raise ValueError(f"lengths of shape {tuple(lengths.shape)}: ({B},) expected")
+    _where(grads, lengths, *dSs)
+    st = load_library().dp_relative_bias_grads(
+        ctx, len(dSs), _table([x.data_ptr() for x in dSs], len(dSs)), _dtype_code(dt), _i32(None if lengths is None else _dense("lengths", lengths)),
+        int(bool(causal)), n, (ctypes.c_int32 * n)(*starts), int(bool(bidirectional)), B, H, Tq, Tk, _f32(_dense("grads", grads)))
+    _check(ctx, st, "dp_relative_bias_grads")
+
+
+def _token_stride(what, x):
+    """Numbers from token to token of [B, T, H, D], whose heads have to lie next to each other and whose tokens have to be evenly spaced."""
+    B, T, H, D = x.shape
+    st = x.stride()
+    ld = st[1] if T > 1 else st[0] if B > 1 else H * D
+    if (x.numel() and (st[3] != 1 or (H > 1 and st[2] != D) or (B > 1 and st[0] != T * ld))):
+        raise ValueError(f"{what}: a token's heads next to each other and tokens evenly spaced expected, got strides {tuple(st)}")
+    return ld if x.numel() else H * D
+
+
+def _qk(q, k, gain_q, gain_k, cos, sin, positions, dense, strided):
+    """The arguments that the two calls share, from q to n_pos and on to the sizes; `dense`, `strided`: further tensors laid out as queries and
+    keys, dense or as q and k."""
+    (B, T, Hq, D), Hk = q.shape, k.shape[2]
+    if tuple(k.shape) != (B, T, Hk, D) or k.dtype != q.dtype:
+        raise ValueError("q [B, T, Hq, D] and k [B, T, Hk, D] of one dtype expected")
+    ldq, ldk = _token_stride("q", q), _token_stride("k", k)
+    for g in (gain_q, gain_k):
+        if tuple(g.shape) != (D,):
+            raise ValueError(f"a gain of shape {tuple(g.shape)}: ({D},) expected")
+    for name, t, like in dense:
+        if t.shape != like.shape or t.dtype != q.dtype:
+            raise ValueError(f"{name}: shape {tuple(like.shape)} and {q.dtype} expected")
+        _dense(name, t)
+    for name, t, like, ld in ((n, t, like, ldq if like is q else ldk) for n, t, like in strided):
+        if t.shape != like.shape or t.dtype != q.dtype or _token_stride(name, t) != ld:
+            raise ValueError(f"{name}: the shape, type and strides of what it is the gradient of expected")
+    if (cos is None) != (sin is None):
+        raise ValueError("cos and sin go together")
+    n_pos = R = 0
+    if cos is not None:
+        n_pos, R = cos.shape[0], 2 * cos.shape[1]
+        if cos.shape != sin.shape:
+            raise ValueError("cos and sin must share one shape")
+        _dense("cos", cos), _dense("sin", sin)
+    if positions is not None and tuple(positions.shape) != (B, T):
+        raise ValueError(f"positions of shape {tuple(positions.shape)}: ({B}, {T}) expected")
+    _where(q, k, gain_q, gain_k, cos, sin, positions, *(x[1] for x in dense), *(x[1] for x in strided))
+    head = (q.data_ptr(), k.data_ptr(), _dtype_of(q), ldq, ldk, _f32(_dense("gain_q", gain_q)), _f32(_dense("gain_k", gain_k)), _f32(cos), _f32(sin), n_pos,
+            _i32(None if positions is None else _dense("positions", positions)))
+    return head, (B, T, Hq, Hk, D, R)
+
+
+def dp_qk_norm(ctx, q, k, gain_q, gain_k, cos, sin, yq, yk, *, positions=None, interleaved=False, eps=1e-6):
+    """q [B, T, Hq, D], k [B, T, Hk, D] (parts of a fused projection's output, if a token's heads lie next to each other), gains [D], cos and
+    sin [positions, R / 2] or None (no rotation); yq, yk: dense, overwritten; positions: int32 [B, T] or None (0 .. T - 1)."""
+    head, sizes = _qk(q, k, gain_q, gain_k, cos, sin, positions, (("yq", yq, q), ("yk", yk, k)), ())
+    st = load_library().dp_qk_norm(ctx, *head, int(bool(interleaved)), *sizes, float(eps), yq.data_ptr(), yk.data_ptr())
+    _check(ctx, st, "dp_qk_norm")
+
+
+def dp_qk_norm_grads(ctx, q, k, gain_q, gain_k, cos, sin, dyq, dyk, grads, dq=None, dk=None, *, positions=None, interleaved=False, eps=1e-6):
+    """dyq, dyk: dense; grads [B, 2, D] float32, overwritten: every example's gradients of the two gains; dq, dk: laid out as q and k,
+    overwritten, or both None."""
+    if (dq is None) != (dk is None):
+        raise ValueError("dq and dk go together")
+    head, sizes = _qk(q, k, gain_q, gain_k, cos, sin, positions, (("dyq", dyq, q), ("dyk", dyk, k)),
+                      (("dq", dq, q), ("dk", dk, k)) if dq is not None else ())
+    if tuple(grads.shape) != (sizes[0], 2, sizes[4]):
+        raise ValueError(f"grads of shape {tuple(grads.shape)}: {(sizes[0], 2, sizes[4])} expected")
+    _where(q, grads)
+    st = load_library().dp_qk_norm_grads(ctx, *head, int(bool(interleaved)), *sizes, float(eps), dyq.data_ptr(), dyk.data_ptr(), _f32(_dense("grads", grads)),
+                                         None if dq is None else dq.data_ptr(), None if dk is None else dk.data_ptr())
+    _check(ctx, st, "dp_qk_norm_grads")
 
 
 def dp_noise_adamw(ctx, params, m, v, sum_, *, n=None, elem_offset=0, sigma, C, seed, step, batch_size, lr, beta1, beta2,

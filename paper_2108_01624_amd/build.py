@@ -14,7 +14,8 @@ LIB_PATH = os.path.join(PKG_DIR, "libdpclip.so")
 NATIVE_PATH = os.path.join(PKG_DIR, "_native.so")
 BUILD_DIR = os.path.join(PKG_DIR, "_build")
 
-SOURCES = ["dp_api.hip", "dp_update.hip", "dp_rowwise.hip", "dp_gram.hip", "dp_wgemm.hip", "dp_tied.hip"]
+SOURCES = ["dp_api.hip", "dp_update.hip", "dp_rowwise.hip", "dp_gram.hip", "dp_wgemm.hip", "dp_tied.hip", "dp_held.hip", "dp_relbias.hip",
+           "dp_qknorm.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-I" + INCLUDE, "-I" + CSRC,

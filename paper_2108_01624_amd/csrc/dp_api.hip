@@ -173,7 +173,7 @@ dp_status dp_sync(dp_ctx* ctx) {
     DP_HIP_CHECK(ctx, hipMemcpy(&w, ctx->err_word, sizeof(int), hipMemcpyDeviceToHost));
     if (w) {
         DP_HIP_CHECK(ctx, hipMemset(ctx->err_word, 0, sizeof(int)));
-        if (w & DP_ERRBIT_INDEX) FAIL(ctx, DP_ERR_INDEX, "a token id outside [0, V) was met on the device");
+        if (w & DP_ERRBIT_INDEX) FAIL(ctx, DP_ERR_INDEX, "a token id outside [0, V), or a position outside its table, was met on the device");
         FAIL(ctx, DP_ERR_VALUE, "a per-example squared norm was NaN or overflowed fp32: the sums it entered hold NaN");
     }
     return DP_OK;
@@ -440,6 +440,214 @@ dp_status dp_clip_factors(dp_ctx* ctx, const float* sqnorms, int B, float C, flo
     if (!(C > 0.f) || !isfinite(C)) FAIL(ctx, DP_ERR_VALUE, "clip norm C must be positive and finite");
     if (B == 0) return DP_OK;
     return dpk_clip_factors(ctx, sqnorms, B, C, c);
+}
+
+// Tensors of held gradients; `out` may be NULL (a call without outputs).
+static dp_status check_grads(dp_ctx* ctx, int n, const void* const* X, const uint64_t* counts, dp_dtype dtype, int B, const float* sqnorms, const void* const* out,
+                             int out_align) {
+    TRY(check_dtype(ctx, dtype));
+    if (n < 0 || B < 0) FAIL(ctx, DP_ERR_SHAPE, "negative count");
+    if (n > 0 && (!X || !counts)) FAIL(ctx, DP_ERR_NULL, "a table is NULL");
+    if (B == 0) return DP_OK;  // (tensors of no elements have no address)
+    const uintptr_t low = dtype == DP_BF16 ? 1 : 3;
+    for (int l = 0; l < n; ++l) {
+        if (counts[l] == 0) continue;
+        if (counts[l] > (1ull << 59) / (uint64_t)B) FAIL(ctx, DP_ERR_SHAPE, "counts[%d] is too large", l);
+        if (!X[l]) FAIL(ctx, DP_ERR_NULL, "X[%d] is NULL", l);
+        if ((uintptr_t)X[l] & low) FAIL(ctx, DP_ERR_ALIGN, "X[%d] is not aligned to its elements", l);
+        if (!out) continue;
+        if (!out[l]) FAIL(ctx, DP_ERR_NULL, "output %d is NULL", l);
+        if ((uintptr_t)out[l] & (uintptr_t)(out_align - 1)) FAIL(ctx, DP_ERR_ALIGN, "output %d is not aligned to its elements", l);
+    }
+    return check_f32(ctx, "sqnorms", sqnorms);
+}
+
+dp_status dp_sqnorms_grads(dp_ctx* ctx, int n_layers, const void* const* X, const uint64_t* counts, dp_dtype dtype, int B, float* sqnorms) {
+    REQUIRE_CTX(ctx);
+    TRY(check_grads(ctx, n_layers, X, counts, dtype, B, sqnorms, nullptr, 1));
+    if (B == 0 || n_layers == 0) return DP_OK;
+    return dpk_held_sqnorms(ctx, n_layers, X, counts, dtype, B, sqnorms);
+}
+
+dp_status dp_clip_accumulate_grads(dp_ctx* ctx, int n_layers, const void* const* X, const uint64_t* counts, dp_dtype dtype, int B, float C,
+                                   const float* sqnorms, float* const* sums) {
+    REQUIRE_CTX(ctx);
+    if (n_layers > 0 && !sums) FAIL(ctx, DP_ERR_NULL, "a table is NULL");
+    TRY(check_grads(ctx, n_layers, X, counts, dtype, B, sqnorms, (const void* const*)sums, 4));
+    TRY(check_clip(ctx, C, 0));
+    if (B == 0 || n_layers == 0) return DP_OK;
+    return dpk_held_sums(ctx, n_layers, X, counts, dtype, B, C, sqnorms, sums);
+}
+
+dp_status dp_clip_grads(dp_ctx* ctx, int n_layers, const void* const* X, const uint64_t* counts, dp_dtype dtype, int B, float C,
+                        const float* sqnorms, void* const* Y) {
+    REQUIRE_CTX(ctx);
+    if (n_layers > 0 && !Y) FAIL(ctx, DP_ERR_NULL, "a table is NULL");
+    TRY(check_grads(ctx, n_layers, X, counts, dtype, B, sqnorms, Y, dtype == DP_BF16 ? 2 : 4));
+    TRY(check_clip(ctx, C, 0));
+    if (B == 0 || n_layers == 0) return DP_OK;
+    return dpk_held_scale(ctx, n_layers, X, counts, dtype, B, C, sqnorms, Y);
+}
+
+// d^m e^j < r^j e^m for whole numbers, n = m >= j, by comparing products of 32-bit words (at most 128 factors of 30 bits: 120 words).
+static bool bucket_below(uint32_t d, uint32_t e, uint32_t r, int m, int j) {
+    uint32_t a[128] = {1}, b[128] = {1};
+    auto times = [](uint32_t* w, uint32_t f) {
+        uint64_t carry = 0;
+        for (int k = 0; k < 128; ++k) {
+            carry += (uint64_t)w[k] * f;
+            w[k] = (uint32_t)carry;
+            carry >>= 32;
+        }
+    };
+    for (int k = 0; k < m; ++k) {
+        times(a, d);
+        times(b, e);
+    }
+    for (int k = 0; k < j; ++k) {
+        times(a, e);
+        times(b, r);
+    }
+    for (int k = 127; k >= 0; --k)
+        if (a[k] != b[k]) return a[k] < b[k];
+    return false;
+}
+
+dp_status dp_relative_buckets(int n, int max_distance, int32_t* starts) {
+    if (!starts) return DP_ERR_NULL;
+    if (n < 2 || n > DP_REL_MAX_SIDE || max_distance <= n / 2 || max_distance > (1 << 30)) return DP_ERR_VALUE;
+    const int e = n / 2, m = n - e;
+    for (int j = 0; j < e; ++j) starts[j] = j;
+    for (int j = 0; j < m; ++j) {
+        int lo = e, hi = max_distance;  // the first distance in [lo, hi] that is not below (at max_distance: 1 >= ..., j < m)
+        while (lo < hi) {
+            const int mid = lo + (hi - lo) / 2;
+            if (bucket_below((uint32_t)mid, (uint32_t)e, (uint32_t)max_distance, m, j)) lo = mid + 1;
+            else hi = mid;
+        }
+        starts[e + j] = lo;
+    }
+    return DP_OK;
+}
+
+static dp_status check_relative(dp_ctx* ctx, int n, const int32_t* starts, dp_dtype dtype, int H, int Tq, int Tk) {
+    TRY(check_dtype(ctx, dtype));
+    if (!starts) FAIL(ctx, DP_ERR_NULL, "starts is NULL");
+    if (n < 1 || n > DP_REL_MAX_SIDE) FAIL(ctx, DP_ERR_SHAPE, "%d buckets: 1 to %d of a side", n, DP_REL_MAX_SIDE);
+    for (int j = 0; j < n; ++j)
+        if (starts[j] < (j ? starts[j - 1] : 0) || starts[j] > (1 << 30) || (j == 0 && starts[0] != 0))
+            FAIL(ctx, DP_ERR_VALUE, "starts[%d] = %d: they begin at 0, do not fall and do not exceed 2^30", j, starts[j]);
+    if (H < 0 || Tq < 0 || Tk < Tq || Tk > (1 << 30)) FAIL(ctx, DP_ERR_SHAPE, "H = %d, Tq = %d, Tk = %d: 0 <= H, 0 <= Tq <= Tk <= 2^30", H, Tq, Tk);
+    return DP_OK;
+}
+
+dp_status dp_relative_bias(dp_ctx* ctx, const float* table, int n, const int32_t* starts, int bidirectional, int H, int Tq, int Tk,
+                           dp_dtype dtype, void* bias) {
+    REQUIRE_CTX(ctx);
+    TRY(check_relative(ctx, n, starts, dtype, H, Tq, Tk));
+    if (H == 0 || Tq == 0) return DP_OK;
+    TRY(check_f32(ctx, "table", table));
+    if (!bias) FAIL(ctx, DP_ERR_NULL, "bias is NULL");
+    if ((uintptr_t)bias & (dtype == DP_BF16 ? 1 : 3)) FAIL(ctx, DP_ERR_ALIGN, "bias is not aligned to its elements");
+    return dpk_relbias(ctx, table, n, starts, bidirectional != 0, H, Tq, Tk, dtype, bias);
+}
+
+dp_status dp_relative_bias_grads(dp_ctx* ctx, int n_layers, const void* const* dS, dp_dtype dtype, const int32_t* lengths, int causal, int n,
+                                 const int32_t* starts, int bidirectional, int B, int H, int Tq, int Tk, float* grads) {
+    REQUIRE_CTX(ctx);
+    TRY(check_relative(ctx, n, starts, dtype, H, Tq, Tk));
+    if (n_layers < 0 || B < 0) FAIL(ctx, DP_ERR_SHAPE, "negative count");
+    if (Tq + Tk - 1 > DP_REL_MAX_LINE) FAIL(ctx, DP_ERR_SHAPE, "Tq + Tk = %d exceeds %d", Tq + Tk, DP_REL_MAX_LINE + 1);
+    if (B == 0 || H == 0) return DP_OK;
+    TRY(check_f32(ctx, "grads", grads));
+    const uint64_t out = (uint64_t)B * H * n * (bidirectional ? 2 : 1);
+    if (n_layers == 0 || Tq == 0) return dpk_zero_f32(ctx, grads, out);
+    if (!dS) FAIL(ctx, DP_ERR_NULL, "a pointer table is NULL");
+    for (int l = 0; l < n_layers; ++l) {
+        if (!dS[l]) FAIL(ctx, DP_ERR_NULL, "dS[%d] is NULL", l);
+        if ((uintptr_t)dS[l] & (dtype == DP_BF16 ? 1 : 3)) FAIL(ctx, DP_ERR_ALIGN, "dS[%d] is not aligned to its elements", l);
+    }
+    if (lengths) TRY(check_f32(ctx, "lengths", lengths));
+    return dpk_relbias_grads(ctx, n_layers, dS, dtype, lengths, causal != 0, n, starts, bidirectional != 0, B, H, Tq, Tk, grads);
+}
+
+// Whether the places of `tokens` tokens, `ld` numbers apart and `width` long, lie in one range of memory with another such tensor's.
+static bool spans_meet(const void* a, long tokens, int64_t lda, long wa, const void* b, int64_t ldb, long wb, size_t elem) {
+    const uintptr_t a0 = (uintptr_t)a, b0 = (uintptr_t)b, a1 = a0 + ((size_t)(tokens - 1) * lda + wa) * elem, b1 = b0 + ((size_t)(tokens - 1) * ldb + wb) * elem;
+    return a && b && a0 < b1 && b0 < a1;
+}
+
+static dp_status check_qk(dp_ctx* ctx, const dp_qk_args& a) {
+    TRY(check_dtype(ctx, a.dtype));
+    TRY(check_bt(ctx, a.B, a.T));
+    if (a.Hq < 0 || a.Hk < 0 || (long)a.Hq + a.Hk > (1 << 20)) FAIL(ctx, DP_ERR_SHAPE, "Hq = %d, Hk = %d: 0 to 2^20 heads", a.Hq, a.Hk);
+    if (a.D < 8 || a.D > 512 || a.D % 8) FAIL(ctx, DP_ERR_SHAPE, "D = %d: a multiple of 8 in [8, 512]", a.D);
+    if (a.R < 0 || a.R > a.D || a.R % 8) FAIL(ctx, DP_ERR_SHAPE, "R = %d: a multiple of 8 in [0, D]", a.R);
+    if (!(a.eps > 0.f) || !isfinite(a.eps)) FAIL(ctx, DP_ERR_VALUE, "eps must be positive and finite");
+    const uintptr_t low = a.dtype == DP_BF16 ? 1 : 3;
+    for (int s = 0; s < 2; ++s) {
+        const int H = s ? a.Hk : a.Hq;
+        const void* x = s ? a.k : a.q;
+        const int64_t ld = s ? a.ldk : a.ldq;
+        if (H == 0 || a.B == 0 || a.T == 0) continue;
+        if (!x) FAIL(ctx, DP_ERR_NULL, "%s is NULL", s ? "k" : "q");
+        if ((uintptr_t)x & low) FAIL(ctx, DP_ERR_ALIGN, "%s is not aligned to its elements", s ? "k" : "q");
+        if (ld < (int64_t)H * a.D || ld > (1ll << 32)) FAIL(ctx, DP_ERR_SHAPE, "%s: tokens %lld numbers apart, %lld are needed", s ? "ldk" : "ldq", (long long)ld, (long long)H * a.D);
+        TRY(check_f32(ctx, s ? "gain_k" : "gain_q", s ? a.gain_k : a.gain_q));
+    }
+    if (a.n_pos < 0) FAIL(ctx, DP_ERR_SHAPE, "negative n_pos");
+    if (a.R > 0 && a.n_pos > 0) {
+        TRY(check_f32(ctx, "cos", a.cos));
+        TRY(check_f32(ctx, "sin", a.sin));
+    }
+    if (a.R > 0 && a.positions) TRY(check_f32(ctx, "positions", a.positions));
+    return DP_OK;
+}
+
+// An output of H heads per token: where it is wanted, aligned and apart from the inputs.
+static dp_status check_qk_out(dp_ctx* ctx, const dp_qk_args& a, const char* name, const void* y, int H, int64_t ld, const void* dyq, const void* dyk) {
+    if (H == 0 || a.B == 0 || a.T == 0) return DP_OK;
+    const size_t e = a.dtype == DP_BF16 ? 2 : 4;
+    const long n = (long)a.B * a.T, D = a.D;
+    if (!y) FAIL(ctx, DP_ERR_NULL, "%s is NULL", name);
+    if ((uintptr_t)y & (e - 1)) FAIL(ctx, DP_ERR_ALIGN, "%s is not aligned to its elements", name);
+    if ((a.Hq && spans_meet(y, n, ld, H * D, a.q, a.ldq, a.Hq * D, e)) || (a.Hk && spans_meet(y, n, ld, H * D, a.k, a.ldk, a.Hk * D, e)) ||
+        (a.Hq && spans_meet(y, n, ld, H * D, dyq, a.Hq * D, a.Hq * D, e)) || (a.Hk && spans_meet(y, n, ld, H * D, dyk, a.Hk * D, a.Hk * D, e)))
+        FAIL(ctx, DP_ERR_VALUE, "%s overlaps an input", name);
+    return DP_OK;
+}
+
+dp_status dp_qk_norm(dp_ctx* ctx, const void* q, const void* k, dp_dtype dtype, int64_t ldq, int64_t ldk, const float* gain_q,
+                     const float* gain_k, const float* cos, const float* sin, int n_pos, const int32_t* positions, int interleaved, int B,
+                     int T, int Hq, int Hk, int D, int R, float eps, void* yq, void* yk) {
+    REQUIRE_CTX(ctx);
+    const dp_qk_args a = {q, k, dtype, ldq, ldk, gain_q, gain_k, cos, sin, n_pos, positions, interleaved != 0, B, T, Hq, Hk, D, R, eps};
+    TRY(check_qk(ctx, a));
+    TRY(check_qk_out(ctx, a, "yq", yq, Hq, (int64_t)Hq * D, nullptr, nullptr));
+    TRY(check_qk_out(ctx, a, "yk", yk, Hk, (int64_t)Hk * D, nullptr, nullptr));
+    if (B == 0 || T == 0 || Hq + Hk == 0) return DP_OK;
+    return dpk_qk_norm(ctx, a, yq, yk);
+}
+
+dp_status dp_qk_norm_grads(dp_ctx* ctx, const void* q, const void* k, dp_dtype dtype, int64_t ldq, int64_t ldk, const float* gain_q,
+                           const float* gain_k, const float* cos, const float* sin, int n_pos, const int32_t* positions, int interleaved,
+                           int B, int T, int Hq, int Hk, int D, int R, float eps, const void* dyq, const void* dyk, float* grads, void* dq,
+                           void* dk) {
+    REQUIRE_CTX(ctx);
+    const dp_qk_args a = {q, k, dtype, ldq, ldk, gain_q, gain_k, cos, sin, n_pos, positions, interleaved != 0, B, T, Hq, Hk, D, R, eps};
+    TRY(check_qk(ctx, a));
+    if (B == 0) return DP_OK;
+    TRY(check_f32(ctx, "grads", grads));
+    if (T == 0 || Hq + Hk == 0) return dpk_zero_f32(ctx, grads, (uint64_t)B * 2 * D);
+    const uintptr_t low = dtype == DP_BF16 ? 1 : 3;
+    if ((Hq && !dyq) || (Hk && !dyk)) FAIL(ctx, DP_ERR_NULL, "dyq or dyk is NULL");
+    if ((Hq && ((uintptr_t)dyq & low)) || (Hk && ((uintptr_t)dyk & low))) FAIL(ctx, DP_ERR_ALIGN, "dyq or dyk is not aligned to its elements");
+    const bool wanted = (Hq && dq) || (Hk && dk);
+    if (wanted) {
+        TRY(check_qk_out(ctx, a, "dq", dq, Hq, ldq, dyq, dyk));
+        TRY(check_qk_out(ctx, a, "dk", dk, Hk, ldk, dyq, dyk));
+    }
+    return dpk_qk_norm_grads(ctx, a, dyq, dyk, grads, dq, dk, wanted);
 }
 
 dp_status dp_clip_accumulate_dense(dp_ctx* ctx, const void* A, const void* G, dp_dtype dtype, int B, int T, int d_in,

@@ -4,6 +4,8 @@
 #include <stdint.h>
 #include <stdio.h>
 
+#include <type_traits>
+
 #include "dpclip.h"
 
 struct dp_prof_rec {
@@ -224,3 +226,28 @@ dp_status dpk_embedding_sums(dp_ctx*, const int32_t* ids, const void* G, dp_dtyp
                              const float* sqnorms, float C, float* sum_E);
 dp_status dpk_tied_cross_sqnorms(dp_ctx*, const int32_t* ids, const void* dY, const void* H, const void* dL, dp_dtype,
                                  int B, int T, int M, int d, int V, float* sqnorms);
+
+// Gradients that the caller holds, n tensors X[l] [B, count[l]].
+dp_status dpk_held_sqnorms(dp_ctx*, int n, const void* const* X, const uint64_t* count, dp_dtype, int B, float* sqnorms);
+dp_status dpk_held_sums(dp_ctx*, int n, const void* const* X, const uint64_t* count, dp_dtype, int B, float C, const float* sqnorms, float* const* sums);
+dp_status dpk_held_scale(dp_ctx*, int n, const void* const* X, const uint64_t* count, dp_dtype, int B, float C, const float* sqnorms, void* const* Y);
+
+// A relative position bias by buckets, n of a side that begin at the distances starts[0 .. n).
+constexpr int DP_REL_MAX_SIDE = 128, DP_REL_MAX_LINE = 32767;  // most buckets of a side; most Tq + Tk - 1 (the diagonals of a plane lie in LDS)
+dp_status dpk_relbias(dp_ctx*, const float* table, int n, const int32_t* starts, int both, int H, int Tq, int Tk, dp_dtype, void* out);
+dp_status dpk_relbias_grads(dp_ctx*, int n_layers, const void* const* dS, dp_dtype, const int32_t* lengths, int causal, int n, const int32_t* starts, int both, int B, int H,
+                            int Tq, int Tk, float* grads);
+
+// Norms of queries and keys with the rotation by position.
+struct dp_qk_args {
+    const void *q, *k;
+    dp_dtype dtype;
+    int64_t ldq, ldk;
+    const float *gain_q, *gain_k, *cos, *sin;
+    int n_pos;
+    const int32_t* positions;
+    int interleaved, B, T, Hq, Hk, D, R;
+    float eps;
+};
+dp_status dpk_qk_norm(dp_ctx*, const dp_qk_args&, void* yq, void* yk);
+dp_status dpk_qk_norm_grads(dp_ctx*, const dp_qk_args&, const void* dyq, const void* dyk, float* grads, void* dq, void* dk, bool wanted);
