@@ -806,6 +806,42 @@ class Context:
         if st != 0:
             self._finish(st, "dp_clip_accumulate_tied_embedding", ids, dY, H, dL, C, sqnorms, sum_E)
 
+    def sqnorms_grads(self, Xs, sqnorms):
+        st = _native.sqnorms_grads(self.handle, Xs, sqnorms)
+        if st != 0:
+            self._finish(st, "dp_sqnorms_grads", Xs, sqnorms)
+
+    def clip_accumulate_grads(self, Xs, C, sqnorms, sums):
+        st = _native.clip_accumulate_grads(self.handle, Xs, C, sqnorms, sums)
+        if st != 0:
+            self._finish(st, "dp_clip_accumulate_grads", Xs, C, sqnorms, sums)
+
+    def clip_grads(self, Xs, C, sqnorms, Ys):
+        st = _native.clip_grads(self.handle, Xs, C, sqnorms, Ys)
+        if st != 0:
+            self._finish(st, "dp_clip_grads", Xs, C, sqnorms, Ys)
+
+    def relative_bias(self, table, starts, bidirectional, bias):
+        st = _native.relative_bias(self.handle, table, starts, bidirectional, bias)
+        if st != 0:
+            self._finish(st, "dp_relative_bias", table, starts, bidirectional, bias)
+
+    def relative_bias_grads(self, dSs, starts, bidirectional, grads, *, lengths=None, causal=False):
+        st = _native.relative_bias_grads(self.handle, dSs, starts, bidirectional, grads, lengths, causal)
+        if st != 0:
+            self._finish(st, "dp_relative_bias_grads", dSs, starts, bidirectional, grads, lengths=lengths, causal=causal)
+
+    def qk_norm(self, q, k, gain_q, gain_k, cos, sin, yq, yk, *, positions=None, interleaved=False, eps=1e-6):
+        st = _native.qk_norm(self.handle, q, k, gain_q, gain_k, cos, sin, yq, yk, positions, interleaved, eps)
+        if st != 0:
+            self._finish(st, "dp_qk_norm", q, k, gain_q, gain_k, cos, sin, yq, yk, positions=positions, interleaved=interleaved, eps=eps)
+
+    def qk_norm_grads(self, q, k, gain_q, gain_k, cos, sin, dyq, dyk, grads, dq=None, dk=None, *, positions=None, interleaved=False, eps=1e-6):
+        st = _native.qk_norm_grads(self.handle, q, k, gain_q, gain_k, cos, sin, dyq, dyk, grads, dq, dk, positions, interleaved, eps)
+        if st != 0:
+            self._finish(st, "dp_qk_norm_grads", q, k, gain_q, gain_k, cos, sin, dyq, dyk, grads, dq, dk, positions=positions,
+                         interleaved=interleaved, eps=eps)
+
     def noise_adamw(self, params, m, v, sum_, *, n=None, elem_offset=0, sigma, C, seed, step, batch_size, lr, beta1, beta2, eps=1e-11,
                     weight_decay, zero_sum=False):
         st = _native.noise_adamw(self.handle, params, m, v, sum_, n, elem_offset, sigma, C, seed, step, batch_size, lr, beta1, beta2, eps,

@@ -16,6 +16,7 @@
 #include <utility>
 #include <vector>
 
+#include <ATen/Context.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "dpclip.h"
@@ -31,6 +32,9 @@ struct Arr {
     int64_t numel = 0;
     int type = OTHER;  // DP_F32, DP_BF16
     bool i32 = false;
+    int64_t st[4] = {0, 0, 0, 0};
+    bool dense = false;
+    int device = -1;  // of a GPU; -1: none
     bool same_shape(const Arr& o) const { return dim == o.dim && !memcmp(s, o.s, sizeof(s)); }
 };
 
@@ -46,6 +50,9 @@ bool get(PyObject* o, Arr& a) {
         const auto st = t.scalar_type();
         a.type = st == at::kFloat ? (int)DP_F32 : st == at::kBFloat16 ? (int)DP_BF16 : OTHER;
         a.i32 = st == at::kInt;
+        for (int k = 0; k < a.dim; ++k) a.st[k] = t.stride(k);
+        a.dense = t.is_contiguous();
+        a.device = t.is_cuda() ? (int)t.get_device() : -1;
         a.p = t.data_ptr();
         return true;
     } catch (...) {
@@ -264,6 +271,163 @@ PyObject* clip_accumulate_tied_embedding(PyObject*, Args a, Py_ssize_t n) {  // 
     ARGS(8);
     NEED(context(a[0], ctx) && t.get_all(a[1], a[2], a[3], a[4]) && num(a[5], C) && get_f32(a[6], sq) && get_f32(a[7], E) && E.numel == t.dL.s[2] * t.dY.s[2]);
     STATUS(t.sums(ctx, C, (float*)sq.p, (float*)E.p));
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// Held gradients, the relative position bias, the norms of queries and keys: dense tensors, all of one call on one GPU
+// ---------------------------------------------------------------------------------------------------------------------
+bool dense_f32(PyObject* o, Arr& a) { return get_f32(o, a) && a.dense; }
+bool dense_data(PyObject* o, Arr& a) { return get_data(o, a) && a.dense; }
+// (Where there is no GPU, nothing can go there.)
+bool beside(const Arr& a, const Arr& b) { return a.device == b.device && (a.device >= 0 || !at::hasCUDA()); }
+
+struct HeldArgs {
+    std::vector<const void*> x;
+    std::vector<uint64_t> counts;
+    std::vector<void*> y;
+    dp_dtype type;
+    int B;
+};
+// Tensors [B, ...] and (outs != NULL) one output of each: sums of a unit's size, or (`whole`) the same type and size.
+bool held(PyObject* Xs, const Arr& sq, PyObject* outs, bool whole, HeldArgs& h) {
+    if (!PyList_CheckExact(Xs) || PyList_GET_SIZE(Xs) == 0 || !sq.dense || sq.dim > 1 || sq.numel < 1 || !fits(sq.numel)) return false;
+    const Py_ssize_t n = PyList_GET_SIZE(Xs);
+    if (!fits(n) || (outs && (!PyList_CheckExact(outs) || PyList_GET_SIZE(outs) != n))) return false;
+    h.B = (int)sq.numel;
+    h.x.reserve(n);
+    h.counts.reserve(n);
+    for (Py_ssize_t k = 0; k < n; ++k) {
+        Arr x, y;
+        if (!dense_data(PyList_GET_ITEM(Xs, k), x) || !beside(x, sq) || (k && x.type != (int)h.type)) return false;
+        if (h.B != 1 && (x.dim == 0 || x.s[0] != h.B)) return false;
+        h.type = (dp_dtype)x.type;
+        h.x.push_back(x.p);
+        h.counts.push_back((uint64_t)(x.numel / h.B));
+        if (!outs) continue;
+        if (!dense_data(PyList_GET_ITEM(outs, k), y) || !beside(y, sq) || y.type != (whole ? x.type : (int)DP_F32) || y.numel != (whole ? x.numel : x.numel / h.B)) return false;
+        h.y.push_back(y.p);
+    }
+    return true;
+}
+
+PyObject* sqnorms_grads(PyObject*, Args a, Py_ssize_t n) {  // ctx, Xs, sqnorms
+    dp_ctx* ctx;
+    Arr sq;
+    HeldArgs h;
+    ARGS(3);
+    NEED(context(a[0], ctx) && get_f32(a[2], sq) && held(a[1], sq, nullptr, false, h));
+    STATUS(dp_sqnorms_grads(ctx, (int)h.x.size(), h.x.data(), h.counts.data(), h.type, h.B, (float*)sq.p));
+}
+
+PyObject* clip_accumulate_grads(PyObject*, Args a, Py_ssize_t n) {  // ctx, Xs, C, sqnorms, sums
+    dp_ctx* ctx;
+    Arr sq;
+    float C;
+    HeldArgs h;
+    ARGS(5);
+    NEED(context(a[0], ctx) && num(a[2], C) && get_f32(a[3], sq) && held(a[1], sq, a[4], false, h));
+    STATUS(dp_clip_accumulate_grads(ctx, (int)h.x.size(), h.x.data(), h.counts.data(), h.type, h.B, C, (float*)sq.p, (float* const*)h.y.data()));
+}
+
+PyObject* clip_grads(PyObject*, Args a, Py_ssize_t n) {  // ctx, Xs, C, sqnorms, Ys
+    dp_ctx* ctx;
+    Arr sq;
+    float C;
+    HeldArgs h;
+    ARGS(5);
+    NEED(context(a[0], ctx) && num(a[2], C) && get_f32(a[3], sq) && held(a[1], sq, a[4], true, h));
+    STATUS(dp_clip_grads(ctx, (int)h.x.size(), h.x.data(), h.counts.data(), h.type, h.B, C, (float*)sq.p, h.y.data()));
+}
+
+bool starts_of(PyObject* o, std::vector<int32_t>& out) {
+    if (!PyList_CheckExact(o) || PyList_GET_SIZE(o) == 0 || PyList_GET_SIZE(o) > 128) return false;
+    out.resize((size_t)PyList_GET_SIZE(o));
+    for (size_t k = 0; k < out.size(); ++k)
+        if (!num(PyList_GET_ITEM(o, k), out[k])) return false;
+    return true;
+}
+
+PyObject* relative_bias(PyObject*, Args a, Py_ssize_t n) {  // ctx, table, starts, bidirectional, bias
+    dp_ctx* ctx;
+    Arr table, bias;
+    std::vector<int32_t> starts;
+    bool both;
+    ARGS(5);
+    NEED(context(a[0], ctx) && dense_f32(a[1], table) && starts_of(a[2], starts) && truth(a[3], both) && dense_data(a[4], bias) && beside(table, bias) && table.dim == 2 &&
+         bias.dim == 3 && fits(bias) && table.s[0] == (int64_t)starts.size() * (both ? 2 : 1) && table.s[1] == bias.s[0]);
+    STATUS(dp_relative_bias(ctx, (float*)table.p, (int)starts.size(), starts.data(), both, (int)bias.s[0], (int)bias.s[1], (int)bias.s[2], (dp_dtype)bias.type, bias.p));
+}
+
+PyObject* relative_bias_grads(PyObject*, Args a, Py_ssize_t n) {  // ctx, dSs, starts, bidirectional, grads, lengths, causal
+    dp_ctx* ctx;
+    std::vector<Arr> dS;
+    Arr grads, lengths;
+    std::vector<int32_t> starts;
+    bool both, causal;
+    ARGS(7);
+    NEED(context(a[0], ctx) && list_of(a[1], dS) && !dS.empty() && starts_of(a[2], starts) && truth(a[3], both) && dense_f32(a[4], grads) && truth(a[6], causal) && grads.dim == 3 &&
+         dS[0].dim == 4 && fits(dS[0]) && dS[0].type != OTHER);
+    const Arr& x = dS[0];
+    for (const Arr& d : dS) NEED(d.dense && d.type == x.type && d.same_shape(x) && beside(d, grads));
+    NEED(grads.s[0] == x.s[0] && grads.s[1] == (int64_t)starts.size() * (both ? 2 : 1) && grads.s[2] == x.s[1]);
+    if (a[5] != Py_None) NEED(get(a[5], lengths) && lengths.i32 && lengths.dense && lengths.dim == 1 && lengths.s[0] == x.s[0] && beside(lengths, grads));
+    const auto p = addresses(dS);
+    STATUS(dp_relative_bias_grads(ctx, (int)p.size(), p.data(), (dp_dtype)x.type, (int32_t*)lengths.p, causal, (int)starts.size(), starts.data(), both, (int)x.s[0], (int)x.s[1],
+                                  (int)x.s[2], (int)x.s[3], (float*)grads.p));
+}
+
+// [B, T, H, D], a token's heads next to each other and its tokens evenly spaced: numbers from token to token.
+bool token_stride(const Arr& x, int64_t& ld) {
+    if (x.dim != 4 || !fits(x) || x.numel == 0) return false;
+    ld = x.s[1] > 1 ? x.st[1] : x.s[0] > 1 ? x.st[0] : x.s[2] * x.s[3];
+    return x.st[3] == 1 && (x.s[2] == 1 || x.st[2] == x.s[3]) && (x.s[0] == 1 || x.st[0] == x.s[1] * ld);
+}
+
+struct QkCall {
+    dp_ctx* ctx;
+    Arr q, k, gq, gk, cos, sin, pos;
+    int64_t ldq, ldk;
+    int R = 0, n_pos = 0;
+    bool inter;
+    float eps;
+    // ctx, q, k, gain_q, gain_k, cos, sin at a; positions, interleaved, eps at z
+    bool read(Args a, Args z) {
+        if (!(context(a[0], ctx) && get_data(a[1], q) && get_data(a[2], k) && token_stride(q, ldq) && token_stride(k, ldk) && q.type == k.type && k.s[0] == q.s[0] && k.s[1] == q.s[1] &&
+              k.s[3] == q.s[3] && beside(q, k) && dense_f32(a[3], gq) && dense_f32(a[4], gk) && gq.dim == 1 && gk.dim == 1 && gq.s[0] == q.s[3] && gk.s[0] == q.s[3] && beside(gq, q) &&
+              beside(gk, q) && truth(z[1], inter) && num(z[2], eps)))
+            return false;
+        if (a[5] != Py_None || a[6] != Py_None) {
+            if (!(dense_f32(a[5], cos) && dense_f32(a[6], sin) && cos.dim == 2 && cos.same_shape(sin) && fits(cos) && cos.s[1] <= 1024 && beside(cos, q) && beside(sin, q))) return false;
+            n_pos = (int)cos.s[0];
+            R = 2 * (int)cos.s[1];
+        }
+        return z[0] == Py_None || (get(z[0], pos) && pos.i32 && pos.dense && pos.dim == 2 && pos.s[0] == q.s[0] && pos.s[1] == q.s[1] && beside(pos, q));
+    }
+    // A dense tensor of the shape and type of q or k; one of its strides.
+    bool like(PyObject* o, Arr& y, const Arr& x) const { return get_data(o, y) && y.dense && y.type == x.type && y.same_shape(x) && beside(y, x); }
+    bool laid_out_like(PyObject* o, Arr& y, const Arr& x, int64_t ld) const {
+        int64_t l;
+        return get_data(o, y) && y.type == x.type && y.same_shape(x) && beside(y, x) && token_stride(y, l) && l == ld;
+    }
+};
+#define QK_HEAD(c) c.ctx, c.q.p, c.k.p, (dp_dtype)c.q.type, c.ldq, c.ldk, (float*)c.gq.p, (float*)c.gk.p, (float*)c.cos.p, (float*)c.sin.p, c.n_pos, (int32_t*)c.pos.p, c.inter
+#define QK_SIZES(c) (int)c.q.s[0], (int)c.q.s[1], (int)c.q.s[2], (int)c.k.s[2], (int)c.q.s[3], c.R, c.eps
+
+PyObject* qk_norm(PyObject*, Args a, Py_ssize_t n) {  // ctx, q, k, gain_q, gain_k, cos, sin, yq, yk, positions, interleaved, eps
+    QkCall c;
+    Arr yq, yk;
+    ARGS(12);
+    NEED(c.read(a, a + 9) && c.like(a[7], yq, c.q) && c.like(a[8], yk, c.k));
+    STATUS(dp_qk_norm(QK_HEAD(c), QK_SIZES(c), yq.p, yk.p));
+}
+
+PyObject* qk_norm_grads(PyObject*, Args a, Py_ssize_t n) {  // ctx, q, k, gain_q, gain_k, cos, sin, dyq, dyk, grads, dq, dk, positions, interleaved, eps
+    QkCall c;
+    Arr dyq, dyk, g, dq, dk;
+    ARGS(15);
+    NEED(c.read(a, a + 12) && c.like(a[7], dyq, c.q) && c.like(a[8], dyk, c.k) && dense_f32(a[9], g) && beside(g, c.q) && g.dim == 3 && g.s[0] == c.q.s[0] && g.s[1] == 2 && g.s[2] == c.q.s[3]);
+    if (a[10] != Py_None || a[11] != Py_None) NEED(c.laid_out_like(a[10], dq, c.q, c.ldq) && c.laid_out_like(a[11], dk, c.k, c.ldk));
+    STATUS(dp_qk_norm_grads(QK_HEAD(c), QK_SIZES(c), dyq.p, dyk.p, (float*)g.p, dq.p, dk.p));
 }
 
 // ctx, params, m, v, sum, n, elem_offset, sigma, C, seed, step, batch_size, lr, beta1, beta2, eps, weight_decay, zero_sum[, snr_sq]
@@ -567,7 +731,8 @@ PyObject* guarded(PyObject* self, Args a, Py_ssize_t n) {
 #define METHOD(name) {#name, (PyCFunction)(void (*)(void))guarded<name>, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(zero_f32), METHOD(sqnorms_dense), METHOD(clip_accumulate_dense), METHOD(sqnorms_dense_batched), METHOD(clip_accumulate_dense_batched),
                          METHOD(sqnorms_embedding), METHOD(clip_accumulate_embedding), METHOD(sqnorms_tied_embedding), METHOD(clip_accumulate_tied_embedding),
-                         METHOD(noise_adamw), METHOD(pass1), METHOD(pass2), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(noise_adamw), METHOD(sqnorms_grads), METHOD(clip_accumulate_grads), METHOD(clip_grads), METHOD(relative_bias),
+                         METHOD(relative_bias_grads), METHOD(qk_norm), METHOD(qk_norm_grads), METHOD(pass1), METHOD(pass2), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
