@@ -240,7 +240,7 @@ dp_status dp_clip_factors(dp_ctx* ctx, const float* sqnorms, int B, float C, flo
  * dp_relative_bias_grads and dp_qk_norm_grads write) or, with B = 1, the whole gradient of one unit that is clipped as such (a user, a
  * micro-batch).  The norms add to those of the other calls of pass 1.  X and counts are HOST arrays, read during the call only; pointers
  * need the alignment of an element only, counts any value; tensors of no elements are passed over, their pointer is not looked at.
- * Tensors of different types go into calls of their own.  Up to 120 tensors share a launch.
+ * Tensors of different types go into calls of their own.  Up to 160 tensors share a launch.  With B > 1 counts end at 2^32 - 16 (DP_ERR_SHAPE above).
  * ------------------------------------------------------------------------------------------------- */
 
 /* sqnorms[i] += sum_l sum_k X[l][i, k]^2.  The norms of a tensor's pieces pass through the workspace (a float per unit for every tensor,

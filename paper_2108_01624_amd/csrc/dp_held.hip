@@ -2,56 +2,75 @@
 // and the scaled gradients.
 //
 // Roofline: HBM.  The norm reads every element once (one multiply-add each); the sums read it again and read and write 4 bytes per
-// entry of the sums; the scaled form reads and writes it.  Rows start wherever n_l puts them: 16-byte accesses are declared with the
+// entry of the sums; the scaled form reads and writes it.  Rows start wherever n_l puts them: wide accesses are declared with the
 // alignment of an element, which the hardware serves at any address.
 #include "dp_common.h"
 
 namespace {
 
-constexpr int HELD_TABLE = 120;     // tensors per launch: their table is a kernel argument, of less than 4 KiB
-constexpr int WAVE_ROW = 4096;      // rows up to this length are one wave's, longer ones one or several workgroups'
-constexpr int SUM_COLS = 64 * 8;    // columns of a workgroup of the sums over several units
-constexpr int FACTORS = 1024;       // clip factors in LDS at a time
+constexpr int HELD_TABLE = 160;          // tensors per launch: their table is a kernel argument, of less than 4 KiB
+constexpr uint64_t HELD_ENTRY = 1ull << 31;  // most elements of an entry of one unit; longer tensors are several entries
+constexpr uint64_t HELD_PIECE = 16384;   // elements of a workgroup of the norms and of the scaled gradients
+constexpr int WAVE_ROW = 4096;           // rows up to this length are one wave's
+constexpr int ADD_COLS = 256 * 4;        // columns of a workgroup of the sums, one unit
+constexpr int SUM_COLS = 64 * 8;         // ... several units
+constexpr uint64_t LAST_LEVEL = 192ull << 20;  // bytes of the 256 MiB behind the L2s that a gradient may count on
+constexpr int FACTORS = 1024;            // clip factors in LDS at a time
 
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
 typedef u32x4_t u32x4_a2 __attribute__((aligned(2)));
+typedef u32x2_t u32x2_a2 __attribute__((aligned(2)));
 typedef f32x4_t f32x4_a4 __attribute__((aligned(4)));
 
-template <bool BF16>
+// Elements from any address of an element.  STREAM: with the non-temporal hint.  The second pass and the sums carry it; the norms do where the
+// gradients are more than the last-level cache keeps for the second pass (164 MB fp32, norms and scaling: 97 us with cached norms, 107 with
+// streamed ones; 668 MB bf16 streamed, norms alone: 98 us, cached 110).
+template <bool BF16, bool STREAM = true>
 struct Held {
     typedef typename std::conditional<BF16, uint16_t, float>::type elem;
-    // eight elements from any address of an element
+    template <typename V>
+    static __device__ __forceinline__ V ld(const V* p) {
+        if constexpr (STREAM) return __builtin_nontemporal_load(p);
+        else return *p;
+    }
+    static __device__ __forceinline__ void load4(const elem* p, float v[4]) {
+        if constexpr (BF16) {
+            const u32x2_t w = ld(reinterpret_cast<const u32x2_a2*>(p));
+            v[0] = dp_bf16_lo(w[0]);
+            v[1] = dp_bf16_hi(w[0]);
+            v[2] = dp_bf16_lo(w[1]);
+            v[3] = dp_bf16_hi(w[1]);
+        } else {
+            const f32x4_t w = ld(reinterpret_cast<const f32x4_a4*>(p));
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[k] = w[k];
+        }
+    }
     static __device__ __forceinline__ void load8(const elem* p, float v[8]) {
         if constexpr (BF16) {
-            const u32x4_t w = *reinterpret_cast<const u32x4_a2*>(p);
+            const u32x4_t w = ld(reinterpret_cast<const u32x4_a2*>(p));
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 v[2 * k] = dp_bf16_lo(w[k]);
                 v[2 * k + 1] = dp_bf16_hi(w[k]);
             }
         } else {
-            const f32x4_t a = *reinterpret_cast<const f32x4_a4*>(p), b = *reinterpret_cast<const f32x4_a4*>(p + 4);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                v[k] = a[k];
-                v[4 + k] = b[k];
-            }
+            load4(p, v);
+            load4(p + 4, v + 4);
         }
     }
     static __device__ __forceinline__ float load1(const elem* p) {
         if constexpr (BF16) return dp_bf16_bits_to_f32(*p);
         else return *p;
     }
-    static __device__ __forceinline__ void store8(elem* p, const float v[8]) {
+    static __device__ __forceinline__ void store4(elem* p, const float v[4]) {
         if constexpr (BF16) {
-            typedef __bf16 bf16x8_a2 __attribute__((ext_vector_type(8), aligned(2)));
-            bf16x8_t w;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) w[k] = (__bf16)v[k];
-            *reinterpret_cast<bf16x8_a2*>(p) = w;
+            typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+            const bf16x4_t w = {(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
+            __builtin_nontemporal_store(__builtin_bit_cast(u32x2_t, w), reinterpret_cast<u32x2_a2*>(p));
         } else {
-            *reinterpret_cast<f32x4_a4*>(p) = f32x4_t{v[0], v[1], v[2], v[3]};
-            *reinterpret_cast<f32x4_a4*>(p + 4) = f32x4_t{v[4], v[5], v[6], v[7]};
+            __builtin_nontemporal_store(f32x4_t{v[0], v[1], v[2], v[3]}, reinterpret_cast<f32x4_a4*>(p));
         }
     }
     static __device__ __forceinline__ void store1(elem* p, float v) {
@@ -62,30 +81,37 @@ struct Held {
 
 // The tensors of a launch.  Workgroups first[l] .. first[l + 1] - 1 are tensor l's.
 struct HeldTable {
-    const void* x[HELD_TABLE];
-    void* y[HELD_TABLE];            // sums or scaled gradients (not used by the norms)
-    uint64_t count[HELD_TABLE];     // elements of a unit
-    int first[HELD_TABLE];
+    uintptr_t x[HELD_TABLE];
+    uintptr_t y[HELD_TABLE];     // sums or scaled gradients; norms: the first of the tensor's partial norms
+    uint32_t count[HELD_TABLE];  // elements of a unit
+    uint32_t first[HELD_TABLE];
     int n;
 };
 
-// The tensor of workgroup b: two entries a lane and two ballots (a search by halves would be seven dependent loads).
-__device__ __forceinline__ int held_tensor(const HeldTable& t, int b) {
-    const int lane = threadIdx.x & 63;
-    const bool lo = lane < t.n && t.first[lane] <= b, hi = lane + 64 < t.n && t.first[lane + 64] <= b;
-    return __builtin_amdgcn_readfirstlane(__popcll(__ballot(lo)) + __popcll(__ballot(hi)) - 1);
+// The tensor of workgroup b: a search by halves over scalar loads.  (Two entries a lane and ballots, one round of vector loads, cost a
+// workgroup of 1,024 columns more than its work: 334 M bf16 elements added to their sums 684 us that way, 503 this way.)
+__device__ __forceinline__ int held_tensor(const HeldTable& t, uint32_t b) {
+    int lo = 0, hi = t.n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (t.first[mid] <= b) lo = mid;
+        else hi = mid;
+    }
+    return __builtin_amdgcn_readfirstlane(lo);
 }
 
-// What of a tensor a workgroup (a wave, for short rows) does: elements [from, to) of unit `unit`, in whole groups of eight but for the last.
+// workgroups of a row that is not one wave's (0: it is)
+__host__ __device__ __forceinline__ uint32_t held_pieces(uint64_t count, uint32_t per) { return count <= WAVE_ROW ? 0 : (uint32_t)((count + per - 1) / per); }
+
+// What of a tensor a workgroup (a wave, for short rows) does: elements [from, to) of a unit's `count`.
 struct HeldPiece {
-    int unit, piece;
-    uint64_t from, to;
+    int unit;
+    uint32_t piece, from, to;
     int lane, lanes;
 };
-__device__ __forceinline__ HeldPiece held_piece(const HeldTable& t, int l, int b, int B, int pieces) {
+__device__ __forceinline__ HeldPiece held_piece(uint32_t count, uint32_t k, int B, uint32_t per) {
     HeldPiece p;
-    const uint64_t count = t.count[l];
-    const int k = b - t.first[l];
+    const uint32_t pieces = held_pieces(count, per);
     if (pieces == 0) {
         p.unit = 4 * k + (threadIdx.x >> 6);
         p.piece = 0;
@@ -96,31 +122,26 @@ __device__ __forceinline__ HeldPiece held_piece(const HeldTable& t, int l, int b
     } else {
         p.unit = k / pieces;
         p.piece = k - p.unit * pieces;
-        const uint64_t per = ((count + 7) / 8 + pieces - 1) / pieces * 8;
-        p.from = per * p.piece < count ? per * p.piece : count;
-        p.to = p.from + per < count ? p.from + per : count;
+        p.from = p.piece * per;
+        p.to = count - p.from < per ? count : p.from + per;
         p.lane = threadIdx.x;
         p.lanes = 256;
     }
     return p;
 }
-// pieces of a row for `per` elements each (0: a wave takes it whole)
-__host__ __device__ __forceinline__ int held_pieces(uint64_t count, uint64_t per) { return count <= WAVE_ROW ? 0 : (int)((count + per - 1) / per); }
 
-// part[unit * J + col[l] + piece] = sum of squares.  Four independent chains a thread.
-struct HeldCols {
-    int col[HELD_TABLE];
-};
-template <bool BF16>
-__global__ __launch_bounds__(256) void held_sqnorms_kernel(HeldTable t, HeldCols cols, int B, uint64_t per, int J, float* __restrict__ part) {
-    typedef Held<BF16> IO;
+// part[unit * J + y[l] + piece] = sum of squares.  Four independent chains a thread, four loads in flight.
+template <bool BF16, bool STREAM>
+__global__ __launch_bounds__(256) void held_sqnorms_kernel(HeldTable t, int B, uint32_t per, uint32_t J, float* __restrict__ part) {
+    typedef Held<BF16, STREAM> IO;
     __shared__ float red[4];
-    const int l = held_tensor(t, blockIdx.x), pieces = held_pieces(t.count[l], per);
-    const HeldPiece p = held_piece(t, l, blockIdx.x, B, pieces);
-    const typename IO::elem* x = (const typename IO::elem*)t.x[l] + (p.to ? (uint64_t)p.unit * t.count[l] : 0);
+    const int l = held_tensor(t, blockIdx.x);
+    const uint32_t count = t.count[l];
+    const HeldPiece p = held_piece(count, blockIdx.x - t.first[l], B, per);
+    const typename IO::elem* x = (const typename IO::elem*)t.x[l] + (uint64_t)p.unit * count + p.from;
     float s[4] = {0.f, 0.f, 0.f, 0.f};
-    const uint64_t whole = p.from + (p.to - p.from) / 8 * 8, step = (uint64_t)p.lanes * 8;
-    uint64_t k = p.from + (uint64_t)p.lane * 8;
+    const uint32_t len = p.to > p.from ? p.to - p.from : 0, whole = len / 8 * 8, step = p.lanes * 8;
+    uint32_t k = p.lane * 8;
     for (; k + 3 * step < whole; k += 4 * step) {
         float v[4][8];
 #pragma unroll
@@ -136,28 +157,34 @@ __global__ __launch_bounds__(256) void held_sqnorms_kernel(HeldTable t, HeldCols
 #pragma unroll
         for (int e = 0; e < 8; ++e) s[e & 3] += v[e] * v[e];
     }
-    if (whole + p.lane < p.to) {
+    if (whole + p.lane < len) {
         const float v = IO::load1(x + whole + p.lane);
         s[0] += v * v;
     }
     float sum = (s[0] + s[1]) + (s[2] + s[3]);
-    if (pieces == 0) {
+    float* out = part + (size_t)p.unit * J + t.y[l] + p.piece;
+    if (p.lanes == 64) {
         sum = dp_wave_sum(sum);
-        if (p.lane == 0 && p.unit < B) part[(size_t)p.unit * J + cols.col[l]] = sum;
+        if (p.lane == 0 && p.unit < B) *out = sum;
     } else {
         sum = dp_block_sum<256>(sum, red);
-        if (threadIdx.x == 0) part[(size_t)p.unit * J + cols.col[l] + p.piece] = sum;
+        if (threadIdx.x == 0) *out = sum;
     }
 }
 
 // sqnorms[i] += the J partial sums of unit i, one workgroup a unit.
-__global__ __launch_bounds__(256) void held_finish_kernel(const float* __restrict__ part, int J, float* __restrict__ sqnorms) {
-    __shared__ float red[4];
+__global__ __launch_bounds__(1024) void held_finish_kernel(const float* __restrict__ part, uint32_t J, float* __restrict__ sqnorms) {
+    __shared__ float red[16];
     const float* p = part + (size_t)blockIdx.x * J;
-    float s = 0.f;
-    for (int k = threadIdx.x; k < J; k += 256) s += p[k];
-    s = dp_block_sum<256>(s, red);
-    if (threadIdx.x == 0) sqnorms[blockIdx.x] += s;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    uint32_t k = threadIdx.x;
+    for (; (uint64_t)k + 3 * 1024 < J; k += 4 * 1024) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) s[u] += p[k + u * 1024];
+    }
+    for (; k < J; k += 1024) s[0] += p[k];
+    const float sum = dp_block_sum<1024>((s[0] + s[1]) + (s[2] + s[3]), red);
+    if (threadIdx.x == 0) sqnorms[blockIdx.x] += sum;
 }
 
 // The clip factor of unit i; `tell`: a norm that has none is reported (by one workgroup of a launch: all units', or its own unit's).
@@ -167,25 +194,28 @@ __device__ __forceinline__ float held_factor(const float* sqnorms, int i, float 
     return c;
 }
 
-// sums[k] += c x[k], one unit: a thread's eight elements.
+// sums[k] += c x[k], one unit.  Four elements a thread, the sums' access the wide one, neighbouring workgroups on neighbouring
+// memory: 334 M bf16 elements 504 us (6.6 TB/s); eight elements a thread 604, two or four times four 548 and 565.
 template <bool BF16>
 __global__ __launch_bounds__(256) void held_add_kernel(HeldTable t, float C, const float* __restrict__ sqnorms, int* __restrict__ err) {
     typedef Held<BF16> IO;
     const int l = held_tensor(t, blockIdx.x);
-    const uint64_t count = t.count[l], k = ((uint64_t)(blockIdx.x - t.first[l]) * 256 + threadIdx.x) * 8;
+    const uint32_t count = t.count[l], k = (blockIdx.x - t.first[l]) * ADD_COLS + threadIdx.x * 4;
     if (k >= count) return;
-    const typename IO::elem* x = (const typename IO::elem*)t.x[l];
-    float* y = (float*)t.y[l];
-    const float c = held_factor(sqnorms, 0, C, err, blockIdx.x == 0 && threadIdx.x == 0);
-    if (k + 8 <= count) {
-        float v[8], s[8];
-        IO::load8(x + k, v);
-        Held<false>::load8(y + k, s);
+    const typename IO::elem* x = (const typename IO::elem*)t.x[l] + k;
+    float* y = (float*)t.y[l] + k;
+    const bool tell = blockIdx.x == 0 && threadIdx.x == 0;
+    if (count - k >= 4) {
+        float v[4], s[4];
+        IO::load4(x, v);
+        Held<false>::load4(y, s);
+        const float c = held_factor(sqnorms, 0, C, err, tell);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) s[e] += c * v[e];
-        Held<false>::store8(y + k, s);
+        for (int e = 0; e < 4; ++e) s[e] += c * v[e];
+        Held<false>::store4(y, s);
     } else {
-        for (uint64_t e = k; e < count; ++e) y[e] += c * IO::load1(x + e);
+        const float c = held_factor(sqnorms, 0, C, err, tell);
+        for (uint32_t e = 0; e < count - k; ++e) y[e] += c * IO::load1(x + e);
     }
 }
 
@@ -196,9 +226,9 @@ __global__ __launch_bounds__(64 * RG) void held_sums_kernel(HeldTable t, int B, 
     __shared__ float fac[FACTORS];
     __shared__ float red[RG][SUM_COLS];
     const int l = held_tensor(t, blockIdx.x), lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const uint64_t count = t.count[l], k0 = (uint64_t)(blockIdx.x - t.first[l]) * SUM_COLS, k = k0 + 8 * lane;
+    const uint32_t count = t.count[l], k0 = (blockIdx.x - t.first[l]) * SUM_COLS, k = k0 + 8 * lane;
     const typename IO::elem* x = (const typename IO::elem*)t.x[l] + k;
-    const int have = k + 8 <= count ? 8 : k < count ? (int)(count - k) : 0;
+    const int have = k >= count ? 0 : count - k < 8 ? (int)(count - k) : 8;
     float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     for (int b0 = 0; b0 < B; b0 += FACTORS) {
         const int nb = B - b0 < FACTORS ? B - b0 : FACTORS;
@@ -237,123 +267,172 @@ __global__ __launch_bounds__(64 * RG) void held_sums_kernel(HeldTable t, int B, 
 #pragma unroll
     for (int e = 0; e < 8; ++e) red[w][8 * lane + e] = s[e];
     __syncthreads();
-    float* y = (float*)t.y[l];
-    for (int j = threadIdx.x; j < SUM_COLS; j += 64 * RG) {
-        if (k0 + j >= count) break;
+    float* y = (float*)t.y[l] + k0;
+    for (uint32_t j = threadIdx.x; j < SUM_COLS && j < count - k0; j += 64 * RG) {
         float a = red[0][j];
 #pragma unroll
         for (int g = 1; g < RG; ++g) a += red[g][j];
-        y[k0 + j] += a;
+        y[j] += a;
     }
 }
 
 // y[i][k] = c_i x[i][k], rounded once; nothing to do in place where c_i is one.
 template <bool BF16>
-__global__ __launch_bounds__(256) void held_scale_kernel(HeldTable t, int B, uint64_t per, float C, const float* __restrict__ sqnorms, int* __restrict__ err) {
+__global__ __launch_bounds__(256) void held_scale_kernel(HeldTable t, int B, uint32_t per, float C, const float* __restrict__ sqnorms, int* __restrict__ err) {
     typedef Held<BF16> IO;
     const int l = held_tensor(t, blockIdx.x);
-    const HeldPiece p = held_piece(t, l, blockIdx.x, B, held_pieces(t.count[l], per));
+    const uint32_t count = t.count[l];
+    const HeldPiece p = held_piece(count, blockIdx.x - t.first[l], B, per);
     if (p.from >= p.to) return;
     const float c = held_factor(sqnorms, p.unit, C, err, p.piece == 0 && p.lane == 0);
-    const typename IO::elem* x = (const typename IO::elem*)t.x[l] + (uint64_t)p.unit * t.count[l];
-    typename IO::elem* y = (typename IO::elem*)t.y[l] + (uint64_t)p.unit * t.count[l];
+    const typename IO::elem* x = (const typename IO::elem*)t.x[l] + (uint64_t)p.unit * count;
+    typename IO::elem* y = (typename IO::elem*)t.y[l] + (uint64_t)p.unit * count;
     if (c == 1.f && x == y) return;
-    const uint64_t whole = p.from + (p.to - p.from) / 8 * 8, step = (uint64_t)p.lanes * 8;
-    for (uint64_t k = p.from + (uint64_t)p.lane * 8; k < whole; k += step) {
-        float v[8];
-        IO::load8(x + k, v);
+    for (uint32_t k = p.from + p.lane * 4; k < p.to; k += p.lanes * 4) {
+        if (p.to - k >= 4) {
+            float v[4];
+            IO::load4(x + k, v);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] *= c;
-        IO::store8(y + k, v);
+            for (int e = 0; e < 4; ++e) v[e] *= c;
+            IO::store4(y + k, v);
+        } else {
+            for (uint32_t e = k; e < p.to; ++e) IO::store1(y + e, c * IO::load1(x + e));
+        }
     }
-    if (whole + p.lane < p.to) IO::store1(y + whole + p.lane, c * IO::load1(x + whole + p.lane));
 }
 
-// Elements a workgroup of the norms and of the scaled gradients takes: 8,192, more where that would be many more workgroups than the chip
-// holds at a time.
-uint64_t held_per(int n, const uint64_t* count, int B) {
-    uint64_t total = 0;
-    for (int l = 0; l < n; ++l) total += count[l];
-    const uint64_t even = total / 4096 * B;
-    return even < 8192 ? 8192 : (even + 7) / 8 * 8;
-}
+bool held_overlap(uintptr_t a, uint64_t na, uintptr_t b, uint64_t nb) { return a < b + nb * sizeof(float) && b < a + na * sizeof(float); }
 
-bool held_overlap(const void* a, uint64_t na, const void* b, uint64_t nb) {
-    return na && nb && (uintptr_t)a < (uintptr_t)b + nb * sizeof(float) && (uintptr_t)b < (uintptr_t)a + na * sizeof(float);
-}
-
-// Launches over the tensors that have elements, as many at a time as a table holds, fit `room` columns of partial norms and a grid, and
-// (sums) do not share a buffer.  blocks(l): workgroups of tensor l; columns(l): its partial norms; go(table, columns' places, grid, columns).
+// The tensors that have elements, one after the other (those of one unit in entries of at most 2^31), into launches of as many as a
+// table holds and a grid can number, sums that share a buffer in launches of their own.
+// blocks(count): workgroups of an entry; columns(count): its partial norms (0: none are wanted); go(table, grid).
 template <typename Blocks, typename Columns, typename Go>
-dp_status held_launches(dp_ctx* ctx, int n, const void* const* X, void* const* Y, const uint64_t* count, bool sums, long room, Blocks blocks, Columns columns, Go go) {
+dp_status held_launches(dp_ctx* ctx, int n, const void* const* X, void* const* Y, const uint64_t* count, int B, int xsize, int ysize, bool sums, Blocks blocks, Columns columns,
+                        Go go) {
     HeldTable t{};
-    HeldCols cols{};
-    long grid = 0, used = 0;
+    uint64_t grid = 0, col = 0;
+    uintptr_t lo = UINTPTR_MAX, hi = 0;  // hull of the sums of a launch: in a flat buffer's order every tensor lies outside it
     auto flush = [&]() -> dp_status {
-        if (!t.n) return DP_OK;
-        const dp_status st = go(t, cols, (unsigned)grid, (int)used);
+        const dp_status st = t.n ? go(t, (unsigned)grid) : DP_OK;
         t.n = 0;
-        grid = used = 0;
+        grid = 0;
+        lo = UINTPTR_MAX;
+        hi = 0;
         return st;
     };
     for (int l = 0; l < n; ++l) {
-        if (!count[l]) continue;
-        const long nb = blocks(count[l]), nc = columns(count[l]);
-        if (nb > 0x7FFFFFFFl) {
-            DP_SET_ERR(ctx, "tensor %d: too many elements for one launch", l);
+        if (B > 1 && count[l] > 0xFFFFFFF0ull) {
+            DP_SET_ERR(ctx, "tensor %d: more than 2^32 - 16 elements of a unit", l);
             return DP_ERR_SHAPE;
         }
-        if (nc > room) {
-            DP_SET_ERR(ctx, "the workspace holds %ld partial norms of a unit, %ld are needed", room, nc);
-            return DP_ERR_WORKSPACE;
+        for (uint64_t done = 0; done < count[l];) {
+            const uint64_t c = B > 1 || count[l] - done <= HELD_ENTRY ? count[l] - done : HELD_ENTRY;
+            const uintptr_t x = (uintptr_t)X[l] + done * xsize, y = Y ? (uintptr_t)Y[l] + done * ysize : 0;
+            const uint64_t nb = blocks(c);
+            if (nb > 0x7FFFFFFFull) {
+                DP_SET_ERR(ctx, "tensor %d: too many elements for one launch", l);
+                return DP_ERR_SHAPE;
+            }
+            bool apart = t.n == HELD_TABLE || grid + nb > 0x7FFFFFFFull;
+            if (sums && !apart && y < hi && y + c * ysize > lo)
+                for (int k = 0; k < t.n && !apart; ++k) apart = held_overlap(t.y[k], t.count[k], y, c);
+            if (apart) {
+                const dp_status st = flush();
+                if (st != DP_OK) return st;
+            }
+            t.x[t.n] = x;
+            t.y[t.n] = Y ? y : (uintptr_t)col;
+            t.count[t.n] = (uint32_t)c;
+            t.first[t.n] = (uint32_t)grid;
+            t.n++;
+            grid += nb;
+            col += columns(c);
+            lo = y < lo ? y : lo;
+            hi = y + c * ysize > hi ? y + c * ysize : hi;
+            done += c;
         }
-        bool shared = false;
-        for (int k = 0; sums && k < t.n && !shared; ++k) shared = held_overlap(t.y[k], t.count[k], Y[l], count[l]);
-        if (t.n == HELD_TABLE || grid + nb > 0x7FFFFFFFl || used + nc > room || shared) {
-            const dp_status st = flush();
-            if (st != DP_OK) return st;
-        }
-        t.x[t.n] = X[l];
-        t.y[t.n] = Y ? Y[l] : nullptr;
-        t.count[t.n] = count[l];
-        t.first[t.n] = (int)grid;
-        cols.col[t.n] = (int)used;
-        t.n++;
-        grid += nb;
-        used += nc;
     }
     return flush();
+}
+
+// workgroups of an entry, and partial norms of a tensor in entries
+uint64_t held_blocks(uint64_t c, uint32_t per, int B) {
+    const uint32_t p = held_pieces(c, per);
+    return p ? (uint64_t)p * B : ((uint64_t)B + 3) / 4;
+}
+uint64_t held_columns(uint64_t c, uint32_t per, int B) {
+    uint64_t j = 0;
+    for (; B == 1 && c > HELD_ENTRY; c -= HELD_ENTRY) j += held_pieces(HELD_ENTRY, per);
+    return c ? j + (held_pieces(c, per) ? held_pieces(c, per) : 1) : j;
 }
 
 }  // namespace
 
 dp_status dpk_held_sqnorms(dp_ctx* ctx, int n, const void* const* X, const uint64_t* count, dp_dtype dt, int B, float* sqnorms) {
-    uint64_t per = held_per(n, count, B);
-    const long room = (long)(ctx->ws_bytes / sizeof(float) / B);
-    for (int l = 0; l < n; ++l)  // a small workspace: longer pieces
-        if (room > 0 && (count[l] + per - 1) / per > (uint64_t)room) per = ((count[l] + room - 1) / room + 7) / 8 * 8;
+    const uint64_t room = ctx->ws_bytes / sizeof(float) / B;
+    const int size = dt == DP_BF16 ? 2 : 4;
+    uint64_t total = 0;
+    for (int l = 0; l < n; ++l) total += count[l];
+    const bool stream = total * B * size > LAST_LEVEL;
+    if (room == 0) {
+        DP_SET_ERR(ctx, "the workspace does not hold a partial norm of %d units", B);
+        return DP_ERR_WORKSPACE;
+    }
+    // Tensors in groups whose partial norms fit the workspace: as a rule one, and one sum at the end.  A tensor that alone has too many
+    // is cut into longer pieces.
     float* part = (float*)ctx->ws;
-    auto blocks = [&](uint64_t c) { const int p = held_pieces(c, per); return p ? (long)p * B : ((long)B + 3) / 4; };
-    auto columns = [&](uint64_t c) { const int p = held_pieces(c, per); return p ? (long)p : 1l; };
-    return held_launches(ctx, n, X, nullptr, count, false, room, blocks, columns, [&](const HeldTable& t, const HeldCols& cols, unsigned grid, int J) {
-        if (dt == DP_BF16) hipLaunchKernelGGL(held_sqnorms_kernel<true>, dim3(grid), dim3(256), 0, ctx->stream, t, cols, B, per, J, part);
-        else hipLaunchKernelGGL(held_sqnorms_kernel<false>, dim3(grid), dim3(256), 0, ctx->stream, t, cols, B, per, J, part);
-        DP_LAUNCH_CHECK(ctx, "held_sqnorms");
-        if (J <= 512) return dpk_finish_partials(ctx, part, B, J, sqnorms);
-        hipLaunchKernelGGL(held_finish_kernel, dim3(B), dim3(256), 0, ctx->stream, part, J, sqnorms);
-        DP_LAUNCH_CHECK(ctx, "held_finish");
-        return DP_OK;
-    });
+    for (int l0 = 0; l0 < n;) {
+        uint32_t per = HELD_PIECE;
+        uint64_t J = 0;
+        int m = 0;
+        for (; l0 + m < n; ++m) {
+            const uint64_t j = held_columns(count[l0 + m], per, B);
+            if (J + j > room) break;
+            J += j;
+        }
+        if (m == 0) {
+            const uint64_t c = count[l0], entry = B == 1 && c > HELD_ENTRY ? HELD_ENTRY : c, pieces = room / ((c + entry - 1) / entry);
+            if (pieces == 0) {
+                DP_SET_ERR(ctx, "the workspace holds %llu partial norms of a unit, tensor %d needs more", (unsigned long long)room, l0);
+                return DP_ERR_WORKSPACE;
+            }
+            per = (uint32_t)(((entry + pieces - 1) / pieces + 7) / 8 * 8);
+            J = held_columns(c, per, B);
+            m = 1;
+        }
+        const uint32_t width = (uint32_t)J;
+        auto blocks = [&](uint64_t c) { return held_blocks(c, per, B); };
+        auto columns = [&](uint64_t c) { return held_columns(c, per, B); };
+        const dp_status st = held_launches(ctx, m, X + l0, nullptr, count + l0, B, size, 4, false, blocks, columns, [&](const HeldTable& t, unsigned grid) {
+            auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, ctx->stream, t, B, per, width, part); };
+            if (dt == DP_BF16 && stream) launch(held_sqnorms_kernel<true, true>);
+            else if (dt == DP_BF16) launch(held_sqnorms_kernel<true, false>);
+            else if (stream) launch(held_sqnorms_kernel<false, true>);
+            else launch(held_sqnorms_kernel<false, false>);
+            DP_LAUNCH_CHECK(ctx, "held_sqnorms");
+            return DP_OK;
+        });
+        if (st != DP_OK) return st;
+        if (width > 512) {
+            hipLaunchKernelGGL(held_finish_kernel, dim3(B), dim3(1024), 0, ctx->stream, part, width, sqnorms);
+            DP_LAUNCH_CHECK(ctx, "held_finish");
+        } else if (width > 0) {
+            const dp_status fin = dpk_finish_partials(ctx, part, B, (int)width, sqnorms);
+            if (fin != DP_OK) return fin;
+        }
+        l0 += m;
+    }
+    return DP_OK;
 }
 
 dp_status dpk_held_sums(dp_ctx* ctx, int n, const void* const* X, const uint64_t* count, dp_dtype dt, int B, float C, const float* sqnorms,
                         float* const* sums) {
-    const uint64_t cols = B == 1 ? 256 * 8 : SUM_COLS;
+    const uint64_t cols = B == 1 ? ADD_COLS : SUM_COLS;
     uint64_t tiles = 0;
     for (int l = 0; l < n; ++l) tiles += (count[l] + cols - 1) / cols;
     const bool tall = tiles < 512 && B >= 64;
-    auto blocks = [&](uint64_t c) { return (long)((c + cols - 1) / cols); };
-    return held_launches(ctx, n, X, (void* const*)sums, count, true, 1l << 40, blocks, [](uint64_t) { return 0l; }, [&](const HeldTable& t, const HeldCols&, unsigned grid, int) {
+    auto blocks = [&](uint64_t c) { return (c + cols - 1) / cols; };
+    return held_launches(ctx, n, X, (void* const*)sums, count, B, dt == DP_BF16 ? 2 : 4, 4, true, blocks, [](uint64_t) { return (uint64_t)0; }, [&](const HeldTable& t, unsigned grid) {
         auto launch = [&](auto kernel, int threads, auto... args) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(threads), 0, ctx->stream, t, args..., C, sqnorms, ctx->err_word); };
         if (B == 1 && dt == DP_BF16) launch(held_add_kernel<true>, 256);
         else if (B == 1) launch(held_add_kernel<false>, 256);
@@ -367,9 +446,10 @@ dp_status dpk_held_sums(dp_ctx* ctx, int n, const void* const* X, const uint64_t
 }
 
 dp_status dpk_held_scale(dp_ctx* ctx, int n, const void* const* X, const uint64_t* count, dp_dtype dt, int B, float C, const float* sqnorms, void* const* Y) {
-    const uint64_t per = held_per(n, count, B);
-    auto blocks = [&](uint64_t c) { const int p = held_pieces(c, per); return p ? (long)p * B : ((long)B + 3) / 4; };
-    return held_launches(ctx, n, X, Y, count, false, 1l << 40, blocks, [](uint64_t) { return 0l; }, [&](const HeldTable& t, const HeldCols&, unsigned grid, int) {
+    const uint32_t per = ADD_COLS;
+    const int size = dt == DP_BF16 ? 2 : 4;
+    auto blocks = [&](uint64_t c) { return held_blocks(c, per, B); };
+    return held_launches(ctx, n, X, Y, count, B, size, size, false, blocks, [](uint64_t) { return (uint64_t)0; }, [&](const HeldTable& t, unsigned grid) {
         if (dt == DP_BF16) hipLaunchKernelGGL(held_scale_kernel<true>, dim3(grid), dim3(256), 0, ctx->stream, t, B, per, C, sqnorms, ctx->err_word);
         else hipLaunchKernelGGL(held_scale_kernel<false>, dim3(grid), dim3(256), 0, ctx->stream, t, B, per, C, sqnorms, ctx->err_word);
         DP_LAUNCH_CHECK(ctx, "held_scale");
