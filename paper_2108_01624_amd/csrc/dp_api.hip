@@ -595,7 +595,7 @@ static dp_status check_qk(dp_ctx* ctx, const dp_qk_args& a) {
         if (ld < (int64_t)H * a.D || ld > (1ll << 32)) FAIL(ctx, DP_ERR_SHAPE, "%s: tokens %lld numbers apart, %lld are needed", s ? "ldk" : "ldq", (long long)ld, (long long)H * a.D);
         TRY(check_f32(ctx, s ? "gain_k" : "gain_q", s ? a.gain_k : a.gain_q));
     }
-    if (a.n_pos < 0) FAIL(ctx, DP_ERR_SHAPE, "negative n_pos");
+    if (a.n_pos < 0 || (a.R > 0 && a.n_pos == 0 && a.B > 0 && a.T > 0)) FAIL(ctx, DP_ERR_SHAPE, "n_pos = %d: a table of positions is needed", a.n_pos);
     if (a.R > 0 && a.n_pos > 0) {
         TRY(check_f32(ctx, "cos", a.cos));
         TRY(check_f32(ctx, "sin", a.sin));
