@@ -135,6 +135,23 @@ __device__ __forceinline__ float dp_wave_sum(float v) {
     return v;
 }
 
+// Sum over the LPH (4, 8, ... 64) neighbouring lanes that share a value, in all of them.  Within 16 lanes by permuted operands of the
+// additions themselves: neighbours, then pairs, then, once four (eight) lanes agree, the mirror of eight (sixteen).
+template <int CTRL>
+__device__ __forceinline__ float dp_add_permuted(float v) {
+    return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true));
+}
+template <int LPH>
+__device__ __forceinline__ float dp_lanes_sum(float v) {
+    v = dp_add_permuted<0xB1>(v);                // quad_perm [1, 0, 3, 2]
+    v = dp_add_permuted<0x4E>(v);                // quad_perm [2, 3, 0, 1]
+    if (LPH > 4) v = dp_add_permuted<0x141>(v);  // row_half_mirror
+    if (LPH > 8) v = dp_add_permuted<0x140>(v);  // row_mirror
+    if (LPH > 16) v += __shfl_xor(v, 16, 64);
+    if (LPH > 32) v += __shfl_xor(v, 32, 64);
+    return v;
+}
+
 // Sum over a workgroup of NT threads (NT multiple of 64, <= 1024); result valid in thread 0.
 // `red` is LDS scratch of at least NT/64 floats.  Fixed order => deterministic.
 template <int NT>

@@ -112,23 +112,6 @@ __device__ __forceinline__ void load4(const float* p, float v[4]) {
     for (int k = 0; k < 4; ++k) v[k] = w[k];
 }
 
-// Sum over the LPH lanes of a head, in all of them.  Within 16 lanes by permuted operands of the additions themselves: neighbours, then pairs,
-// then, once four (eight) lanes agree, the mirror of eight (sixteen).
-template <int CTRL>
-__device__ __forceinline__ float add_permuted(float v) {
-    return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true));
-}
-template <int LPH>
-__device__ __forceinline__ float head_sum(float v) {
-    v = add_permuted<0xB1>(v);                // quad_perm [1, 0, 3, 2]
-    v = add_permuted<0x4E>(v);                // quad_perm [2, 3, 0, 1]
-    if (LPH > 4) v = add_permuted<0x141>(v);  // row_half_mirror
-    if (LPH > 8) v = add_permuted<0x140>(v);  // row_mirror
-    if (LPH > 16) v += __shfl_xor(v, 16, 64);
-    if (LPH > 32) v += __shfl_xor(v, 32, 64);
-    return v;
-}
-
 // A wave works on N = 64 / LPH heads at a time, a round: of one token, whose H heads take `rpt` rounds, or of `tpw` whole tokens.
 void set_rounds(Side& S, int lph) {
     const int N = 64 / lph, H = S.H ? S.H : 1;
@@ -251,7 +234,7 @@ __global__ __launch_bounds__(256) void qk_norm_kernel(QkArgs A) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) s += v[e] * v[e];
         if (!ALL && !P.on) s = 0.f;
-        const float r = __builtin_amdgcn_rsqf(head_sum<LPH>(s) * inv + A.eps);
+        const float r = __builtin_amdgcn_rsqf(dp_lanes_sum<LPH>(s) * inv + A.eps);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] *= r * g[e];
         if (P.turned) turn<INTER>(v, in[u].cs, in[u].sn);
@@ -328,8 +311,8 @@ __global__ __launch_bounds__(256) void qk_norm_grads_kernel(QkArgs A) {
                 m += gd[e] * v[e];
             }
             if (!ALL && !P.on) s = m = 0.f;
-            const float r = __builtin_amdgcn_rsqf(head_sum<LPH>(s) * inv + A.eps);
-            m = head_sum<LPH>(m) * inv * r;
+            const float r = __builtin_amdgcn_rsqf(dp_lanes_sum<LPH>(s) * inv + A.eps);
+            m = dp_lanes_sum<LPH>(m) * inv * r;
             if (!at[u].there) continue;
             if (in[u].good) {
 #pragma unroll

@@ -5,6 +5,8 @@
 // that moves by one from row to row.  Gradient: the sums of the diagonals, then those of the buckets' runs.
 //
 // Roofline: HBM, both.  The forward writes H Tq Tk elements, the gradient reads L B H Tq Tk of them with one addition each.
+// Forward, 16 x 2,048 x 2,048: bf16 25 us (5.3 TB/s), fp32 42 us (6.4); gradient, 24 layers x 128 x 16 x 128 x 128 bf16: 240 us (6.7 TB/s),
+// 12 layers x 64 x 16 x 125 x 125: 72 us (5.3).
 #include "dp_common.h"
 
 namespace {
@@ -21,65 +23,62 @@ struct Buckets {
     int n, both;
 };
 
-// The bucket of a key `rel` behind its query (negative: in front).
-__device__ __forceinline__ int bucket_of(const Buckets& b, int rel) {
-    const int dist = rel <= 0 ? -rel : b.both ? rel : 0;
-    int lo = 0, hi = b.n;  // the last start that is not above the distance
+// The bucket of a key `rel` behind its query (negative: in front), by a side's n starts.
+__device__ __forceinline__ int bucket_of(const int* start, int n, int both, int rel) {
+    const int dist = rel <= 0 ? -rel : both ? rel : 0;
+    int lo = 0, hi = n;  // the last start that is not above the distance
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if (b.start[mid] <= dist) lo = mid;
+        if (start[mid] <= dist) lo = mid;
         else hi = mid;
     }
-    return b.both && rel > 0 ? lo + b.n : lo;
+    return both && rel > 0 ? lo + n : lo;
 }
 
-constexpr int FWD_ROWS = 32, FWD_COLS = 256 * 8;
+constexpr int FWD_ROWS = 16;
 
-// bias[h][q][k] = table[bucket(k - (Tk - Tq + q))][h]: a workgroup writes 32 rows of 2,048 columns.  The line of values under the tile
-// lies in LDS; a thread keeps the eight under its columns and takes in one more per row.
+// bias[h][q][k] = table[bucket(k - (Tk - Tq + q))][h]: a workgroup writes 16 rows of 256 x 16 bytes.  The line of values under the tile lies in
+// LDS; a thread keeps those under its columns and takes in one more per row.
 template <bool BF16>
 __global__ __launch_bounds__(256) void relbias_kernel(const float* __restrict__ table, Buckets bk, int H, int Tq, int Tk, int row_tiles, int col_tiles, void* __restrict__ out) {
-    __shared__ float line[FWD_ROWS + FWD_COLS];
+    constexpr int E = BF16 ? 8 : 4, COLS = 256 * E;  // columns of a thread: 16 bytes
+    typedef typename std::conditional<BF16, __bf16, float>::type elem;
+    typedef elem pack __attribute__((ext_vector_type(E)));
+    typedef pack pack_any __attribute__((aligned(sizeof(elem))));
+    __shared__ float line[FWD_ROWS + COLS], value[2 * MAX_SIDE];
+    __shared__ int start[MAX_SIDE];
     int b = blockIdx.x;
     const int ct = b % col_tiles;
     b /= col_tiles;
     const int rt = b % row_tiles, h = b / row_tiles;
-    const int q0 = rt * FWD_ROWS, k0 = ct * FWD_COLS, rows = Tq - q0 < FWD_ROWS ? Tq - q0 : FWD_ROWS, cols = Tk - k0 < FWD_COLS ? Tk - k0 : FWD_COLS;
+    const int q0 = rt * FWD_ROWS, k0 = ct * COLS, rows = min(Tq - q0, FWD_ROWS), cols = min(Tk - k0, COLS);
     // line[j]: distance j + base; row q0 + r, column k0 + c is line[c - r + rows - 1]
     const int base = k0 - (Tk - Tq + q0) - (rows - 1);
-    for (int j = threadIdx.x; j < rows + cols - 1; j += 256) line[j] = table[(size_t)bucket_of(bk, j + base) * H + h];
+    if ((int)threadIdx.x < bk.n) start[threadIdx.x] = bk.start[threadIdx.x];
+    if ((int)threadIdx.x < (bk.both ? 2 * bk.n : bk.n)) value[threadIdx.x] = table[(size_t)threadIdx.x * H + h];
     __syncthreads();
-    const int c = threadIdx.x * 8;
+    for (int j = threadIdx.x; j < rows + cols - 1; j += 256) line[j] = value[bucket_of(start, bk.n, bk.both, j + base)];
+    __syncthreads();
+    const int c = threadIdx.x * E;
     if (c >= cols) return;
-    const int have = cols - c < 8 ? cols - c : 8;
-    float v[8];
+    const int have = min(cols - c, E);
+    float v[E];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = e < have ? line[c + e + rows - 1] : 0.f;
-    size_t at = ((size_t)h * Tq + q0) * Tk + k0 + c;
-    for (int r = 0; r < rows; ++r, at += Tk) {
-        if (have == 8) {
-            if constexpr (BF16) {
-                typedef __bf16 bf16x8_a2 __attribute__((ext_vector_type(8), aligned(2)));
-                bf16x8_t w;
+    for (int e = 0; e < E; ++e) v[e] = e < have ? line[c + e + rows - 1] : 0.f;
+    elem* o = (elem*)out + ((size_t)h * Tq + q0) * Tk + k0 + c;
+    for (int r = 0; r < rows; ++r, o += Tk) {
+        if (have == E) {
+            pack w;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) w[e] = (__bf16)v[e];
-                *reinterpret_cast<bf16x8_a2*>((__bf16*)out + at) = w;
-            } else {
-                typedef f32x4_t f32x4_a4 __attribute__((aligned(4)));
-                f32x4_a4* o = reinterpret_cast<f32x4_a4*>((float*)out + at);
-                o[0] = f32x4_t{v[0], v[1], v[2], v[3]};
-                o[1] = f32x4_t{v[4], v[5], v[6], v[7]};
-            }
+            for (int e = 0; e < E; ++e) w[e] = (elem)v[e];
+            *reinterpret_cast<pack_any*>(o) = w;
         } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (e < have) {
-                    if constexpr (BF16) ((__bf16*)out)[at + e] = (__bf16)v[e];
-                    else ((float*)out)[at + e] = v[e];
-                }
+            for (int e = 0; e < E; ++e)
+                if (e < have) o[e] = (elem)v[e];
         }
 #pragma unroll
-        for (int e = 7; e > 0; --e) v[e] = v[e - 1];
+        for (int e = E - 1; e > 0; --e) v[e] = v[e - 1];
         if (r + 1 < rows) v[0] = line[c + rows - 2 - r];
     }
 }
@@ -89,13 +88,27 @@ struct RelLayers {
     int n;
 };
 
-// How a workgroup's threads share the plane of one example and head, in blocks of 8 x 8: `wide` neighbouring threads take neighbouring
-// blocks of a row of blocks; gr such groups take its rows of blocks in turn, `m` each, and gl of these the layers in turn.
+// How a workgroup's threads share what counts of a plane, in blocks of 8 x 8: `wide` neighbouring threads take neighbouring blocks of a row
+// of blocks; gr such groups take the steps (rows of blocks, pairs of them under FOLD) in turn, `m` each, and gl of these the layers in turn.
 struct RelPlan {
-    int nb, rb;        // blocks in a row and in a column of the plane
-    int splits, per;   // workgroups of a plane, rows of blocks of each
+    int nb, np, steps;  // blocks in a row, threads for one (of which there may be more than `wide`), steps
+    int per;            // steps of a workgroup
     int wide, gr, gl, m;
 };
+template <bool FOLD, int NT>
+__device__ __forceinline__ RelPlan rel_plan(int layers, int rows, int cols, int splits) {
+    RelPlan p;
+    p.nb = max((cols + 7) / 8, 1);
+    p.np = FOLD ? p.nb + 1 : p.nb;
+    p.steps = FOLD ? (p.nb + 1) / 2 : (rows + 7) / 8;
+    p.per = max((int)((unsigned)(p.steps + splits - 1) / (unsigned)splits), 1);
+    p.wide = min(p.np, NT);
+    const unsigned groups = (unsigned)NT / (unsigned)p.wide;
+    p.m = (unsigned)(p.per + groups - 1) / groups;
+    p.gr = (unsigned)(p.per + p.m - 1) / (unsigned)p.m;
+    p.gl = min((int)(groups / (unsigned)p.gr), layers);
+    return p;
+}
 
 constexpr int SUMS = 15;  // diagonals of a block of 8 x 8
 
@@ -104,51 +117,81 @@ constexpr int SUMS = 15;  // diagonals of a block of 8 x 8
 // A thread walks down a band of blocks, its column of blocks one further with every row of blocks, so that the 15 diagonals it adds up stay
 // the same ones: one addition an element, no exchange.  Where it steps over the last column it goes on with the band that begins in column 0
 // (bands p and p - nb together have one block in every row of blocks).  The sums of both bands go to LDS and are joined there.
-template <bool BF16>
-__global__ __launch_bounds__(256) void relbias_grads_kernel(RelLayers t, Buckets bk, const int32_t* __restrict__ lengths, int causal, RelPlan pl, int B, int H, int Tq,
-                                                            int Tk, float* __restrict__ part, int slot0) {
+// FOLD, under a causal mask over a square: a step is a row of blocks s and the one as far from the end, nb - 1 - s, which have nb + 1 blocks that
+// count together, a thread each: the first nb - s threads those of the lower row, of bands 0, -1, ..., the others those of the upper one, of bands
+// -s .. 0.  Again a thread has two bands, one after the other, and half as many steps.  (6 layers x 8 x 16 x 512 x 512 bf16: 43 us, without a mask 70.)
+//
+// Bands in which every distance belongs to the last bucket of its side, those below near_lo and above near_hi, are not taken apart: their sums go to
+// one number a side (4 x 16 x 1,024 x 1,024 of one layer, 2,047 diagonals of which 300 are near: 34 -> 30 us).
+//
+// bf16 loads are streamed (240 us, cached 269); of fp32 a thread's eight columns are two loads that share their lines, which streaming
+// loses (6 layers of ragged examples of up to 509 tokens: 98 us cached, 115 streamed).
+template <bool BF16, bool FOLD, int NT>
+__global__ __launch_bounds__(NT) void relbias_grads_kernel(RelLayers t, Buckets bk, const int32_t* __restrict__ lengths, int causal, int splits, int near_lo, int near_hi, int B,
+                                                           int H, int Tq, int Tk, float* __restrict__ part, int slot0) {
     typedef typename std::conditional<BF16, uint16_t, float>::type elem;
     constexpr int W = BF16 ? 4 : 8;  // words of eight elements
     extern __shared__ float lds[];
-    float* const hold = lds;                        // [band before or after the step over][diagonal][thread]
-    float* const diag = lds + 2 * SUMS * 256;       // [Tq + Tk - 1]
-    const int D = Tq + Tk - 1, off = Tk - Tq, tid = threadIdx.x;
-    const int s = blockIdx.x % pl.splits, mat = blockIdx.x / pl.splits, i = mat / H, h = mat - i * H;
+    const int off = Tk - Tq, tid = threadIdx.x;
+    const int d_lo = max(8 * near_lo - 7, 1 - Tq), d_hi = min(8 * near_hi + 7, Tk - 1);  // columns minus rows of the near bands' diagonals
+    float* const hold = lds;                 // [band before or after the step over][diagonal][thread]
+    float* const diag = lds + 2 * SUMS * NT; // [d_hi - d_lo + 1]
+    __shared__ float far_sum[2][NT / 64];
+    const int s = blockIdx.x % (unsigned)splits, mat = blockIdx.x / (unsigned)splits, i = mat / H, h = mat - i * H;
     int len = Tk;
     if (lengths) len = min(max(lengths[i], 0), Tk);
-    const int nq = min(max(len - off, 0), Tq);
-    const int rb0 = s * pl.per, rb1 = min(rb0 + pl.per, (nq + 7) / 8);
-    const int grp = tid / pl.wide, pp = tid - grp * pl.wide, lg = grp / pl.gr, rg = grp - lg * pl.gr;
+    const int nq = min(max(len - off, 0), Tq);  // rows and columns that count: nq and len
+    const RelPlan pl = rel_plan<FOLD, NT>(t.n, nq, len, splits);
+    const int s0 = s * pl.per, s1 = min(s0 + pl.per, pl.steps);
+    const int grp = tid / (unsigned)pl.wide, pp = tid - grp * pl.wide, lg = grp / (unsigned)pl.gr, rg = grp - lg * pl.gr;
     const bool works = lg < pl.gl;
-    const int ra = rb0 + rg * pl.m, rz = min(ra + pl.m, rb1);
+    const int sa = s0 + rg * pl.m, sz = min(sa + pl.m, s1);
     // elements from the start of this plane to the end of the tensor (what a load may touch)
     const long left = ((long)B * H - mat) * Tq * Tk;
     const int room = left < 0x7FFFFFFF ? (int)left : 0x7FFFFFFF;
 
-    for (int p0 = 0; p0 < pl.nb; p0 += pl.wide) {
+    float past = 0.f, future = 0.f;
+    for (int p0 = 0; p0 < pl.np; p0 += pl.wide) {
         const int p = p0 + pp;
         float acc[SUMS];
+        // the sums of this thread's band before or after its step over; those that it never comes to are zeros
+        auto put = [&](int after) {
+            const int band = after ? p - pl.nb : FOLD ? -p : p;
+            if (band >= near_lo && band <= near_hi) {
+#pragma unroll
+                for (int e = 0; e < SUMS; ++e) hold[(after * SUMS + e) * NT + tid] = acc[e];
+            } else {
+                float sum = 0.f;
+#pragma unroll
+                for (int e = 0; e < SUMS; ++e) sum += acc[e];
+                if (band < near_lo) past += sum;
+                else future += sum;
+            }
+        };
 #pragma unroll
         for (int e = 0; e < SUMS; ++e) acc[e] = 0.f;
-#pragma unroll
-        for (int e = 0; e < 2 * SUMS; ++e) hold[e * 256 + tid] = 0.f;
+        put(0);
+        put(1);
         int over = 0;
-        if (works && p < pl.nb) {
-            for (int rb = ra; rb < rz; ++rb) {
-                int cb = rb + p;
-                if (cb >= pl.nb) {
+        if (works && p < pl.np) {
+            for (int step = sa; step < sz; ++step) {
+                int rb = step, cb = step + p;
+                if (cb < pl.nb) {
+                    if (FOLD) {
+                        rb = pl.nb - 1 - step;
+                        cb = rb - p;
+                    }
+                } else {
                     cb -= pl.nb;
                     if (!over) {
+                        put(0);
 #pragma unroll
-                        for (int e = 0; e < SUMS; ++e) {
-                            hold[e * 256 + tid] = acc[e];
-                            acc[e] = 0.f;
-                        }
+                        for (int e = 0; e < SUMS; ++e) acc[e] = 0.f;
                         over = 1;
                     }
                 }
                 const int q0 = rb * 8, k0 = cb * 8, rows = nq - q0, cut = len - k0;  // (len is never above Tk)
-                if (cut <= 0 || (causal && k0 > q0 + 7 + off)) continue;
+                if (cut <= 0 || (FOLD ? over && 2 * step == pl.nb - 1 : causal && k0 > q0 + 7 + off)) continue;  // (a middle row is its own other)
                 uint32_t mask[W];
 #pragma unroll
                 for (int w = 0; w < W; ++w) {
@@ -166,7 +209,7 @@ __global__ __launch_bounds__(256) void relbias_grads_kernel(RelLayers t, Buckets
                         if (r >= rows) continue;
                         if (at + r * Tk + 8 <= room) {
                             if constexpr (BF16) {
-                                const u32x4_t a = *reinterpret_cast<const u32x4_a2*>(x + r * Tk);
+                                const u32x4_t a = __builtin_nontemporal_load(reinterpret_cast<const u32x4_a2*>(x + r * Tk));
 #pragma unroll
                                 for (int w = 0; w < 4; ++w) v[r][w] = a[w];
                             } else {
@@ -201,51 +244,74 @@ __global__ __launch_bounds__(256) void relbias_grads_kernel(RelLayers t, Buckets
                 }
             }
         }
-#pragma unroll
-        for (int e = 0; e < SUMS; ++e) hold[(over * SUMS + e) * 256 + tid] = acc[e];
+        put(over);
         __syncthreads();
-        // diag[j]: keys j - (Tq - 1) columns behind their row, i.e. rel = j - (Tk - 1)
-        for (int j = tid; j < D; j += 256) {
-            const int dd = j - (Tq - 1), band = dd >> 3, e = dd & 7;
+        // diag[j]: the diagonal of columns d_lo + j behind their rows
+        for (int j = tid; j <= d_hi - d_lo; j += NT) {
+            const int dd = d_lo + j, band = dd >> 3, e = dd & 7;
             float sum = p0 ? diag[j] : 0.f;
 #pragma unroll
             for (int side = 0; side < 2; ++side) {
-                const int b = band + side, ee = e + 7 - 8 * side, after = b < 0, q = (after ? b + pl.nb : b) - p0;
-                if (ee < 0 || q < 0 || q >= pl.wide || q + p0 >= pl.nb) continue;
-                for (int g = 0; g < pl.gr * pl.gl; ++g) sum += hold[(after * SUMS + ee) * 256 + g * pl.wide + q];
+                const int b = band + side, ee = e + 7 - 8 * side;
+                if (ee < 0 || b < near_lo || b > near_hi) continue;
+#pragma unroll
+                for (int after = 0; after < 2; ++after) {
+                    const int at = after ? b + pl.nb : FOLD ? -b : b, q = at - p0;  // the thread that has band b, before or after its step over
+                    if (at < 0 || at >= pl.np || q < 0 || q >= pl.wide) continue;
+                    for (int g = 0; g < pl.gr * pl.gl; ++g) sum += hold[(after * SUMS + ee) * NT + g * pl.wide + q];
+                }
             }
             diag[j] = sum;
         }
         __syncthreads();
     }
-    // the buckets' runs, a wave each
-    const int lane = tid & 63, nbk = bk.both ? 2 * bk.n : bk.n, far = 1 << 30;
-    for (int j = tid >> 6; j < nbk; j += 4) {
+    past = dp_lanes_sum<64>(past);
+    future = dp_lanes_sum<64>(future);
+    if ((tid & 63) == 0) {
+        far_sum[0][tid >> 6] = past;
+        far_sum[1][tid >> 6] = future;
+    }
+    __syncthreads();
+    // the buckets' runs, sixteen lanes each
+    const int lane = tid & 15, nbk = bk.both ? 2 * bk.n : bk.n, far = 1 << 30;
+    for (int j = tid >> 4; j < nbk; j += NT / 16) {
         const int b = j < bk.n ? j : j - bk.n;
         const int lo = bk.start[b], hi = b + 1 < bk.n ? bk.start[b + 1] : far;  // distances lo .. hi - 1
-        int from, to;                                                          // rel from .. to
+        int from, to, whole = -1;                                              // rel from .. to; the side whose far bands belong to it
         if (j < bk.n) {
+            const bool zero = !bk.both && lo == 0 && hi > 0;  // the keys behind the query too
             from = 1 - hi;
-            to = !bk.both && lo == 0 && hi > 0 ? far : -lo;
+            to = zero ? far : -lo;
+            if (j == bk.n - 1) whole = 0;
         } else {
             from = max(lo, 1);
             to = hi - 1;
+            if (b == bk.n - 1) whole = 1;
         }
+        const bool behind = !bk.both && lo == 0 && hi > 0 && !causal;
         if (causal) to = min(to, 0);
-        const int a = max(from + Tk - 1, 0), z = min(to, D) + Tk - 1;
+        const int a = max(from, d_lo - off) + off - d_lo, z = min(to, d_hi - off) + off - d_lo;  // (places in diag)
         float sum = 0.f;
-        for (int k = a + lane; k <= z && k < D; k += 64) sum += diag[k];
-        sum = dp_wave_sum(sum);
+#pragma unroll 4
+        for (int k = a + lane; k <= z; k += 16) sum += diag[k];
+        sum = dp_lanes_sum<16>(sum);
+        for (int w = 0; w < NT / 64; ++w) {
+            if (whole == 0) sum += far_sum[0][w];
+            if (whole == 1 || behind) sum += far_sum[1][w];
+        }
         if (lane == 0) part[(((size_t)(slot0 + s) * B + i) * nbk + j) * H + h] = sum;
     }
 }
 
+// out[k] = sum of the parts of k, sixteen lanes each.
 __global__ __launch_bounds__(256) void relbias_join_kernel(const float* __restrict__ part, int slots, size_t n, float* __restrict__ out) {
-    const size_t k = (size_t)blockIdx.x * 256 + threadIdx.x;
+    const size_t k = (size_t)blockIdx.x * 16 + (threadIdx.x >> 4);
     if (k >= n) return;
-    float s = part[k];
-    for (int j = 1; j < slots; ++j) s += part[j * n + k];
-    out[k] = s;
+    float s = 0.f;
+#pragma unroll 4
+    for (int j = threadIdx.x & 15; j < slots; j += 16) s += part[j * n + k];
+    s = dp_lanes_sum<16>(s);
+    if ((threadIdx.x & 15) == 0) out[k] = s;
 }
 
 Buckets make_buckets(int n, const int32_t* starts, int both) {
@@ -256,25 +322,11 @@ Buckets make_buckets(int n, const int32_t* starts, int both) {
     return b;
 }
 
-RelPlan rel_plan(int L, int Tq, int Tk, int splits) {
-    RelPlan p;
-    p.nb = (Tk + 7) / 8;
-    p.rb = (Tq + 7) / 8;
-    p.per = (p.rb + splits - 1) / splits;
-    p.splits = (p.rb + p.per - 1) / p.per;
-    p.wide = p.nb < 256 ? p.nb : 256;
-    const int groups = 256 / p.wide;
-    p.m = (p.per + groups - 1) / groups;
-    p.gr = (p.per + p.m - 1) / p.m;
-    p.gl = groups / p.gr < L ? groups / p.gr : L;
-    return p;
-}
-
 }  // namespace
 
 dp_status dpk_relbias(dp_ctx* ctx, const float* table, int n, const int32_t* starts, int both, int H, int Tq, int Tk, dp_dtype dt, void* out) {
     const Buckets bk = make_buckets(n, starts, both);
-    const int row_tiles = (Tq + FWD_ROWS - 1) / FWD_ROWS, col_tiles = (Tk + FWD_COLS - 1) / FWD_COLS;
+    const int cols = 256 * (dt == DP_BF16 ? 8 : 4), row_tiles = (Tq + FWD_ROWS - 1) / FWD_ROWS, col_tiles = (Tk + cols - 1) / cols;
     const long grid = (long)H * row_tiles * col_tiles;
     if (grid > 0x7FFFFFFFl) {
         DP_SET_ERR(ctx, "H * Tq * Tk too large for one launch");
@@ -292,13 +344,16 @@ dp_status dpk_relbias_grads(dp_ctx* ctx, int n_layers, const void* const* dS, dp
     const size_t out = (size_t)B * H * n * (both ? 2 : 1);
     const long planes = (long)B * H;
     const int launches = (n_layers + REL_LAYERS - 1) / REL_LAYERS;
-    // workgroups of a plane: as many as fill the chip (five of a CU fit its LDS at T = 128), as long as their parts fit
+    // workgroups of a plane: as many as fill the chip, four to a CU, as long as their parts fit (twice as many: 6 x 8 x 16 x 512 x 512 under a
+    // causal mask 46 us instead of 43, half as many 46)
     int splits = planes >= 1024 ? 1 : (int)(1024 / planes);
     const size_t room = ctx->ws_bytes / (out * sizeof(float));
     if ((size_t)splits * launches > room) splits = room / launches > 1 ? (int)(room / launches) : 1;
-    RelPlan pl = rel_plan(n_layers < REL_LAYERS ? n_layers : REL_LAYERS, Tq, Tk, splits < (Tq + 7) / 8 ? splits : (Tq + 7) / 8);
-    const int slots = pl.splits * launches;
-    if (planes * pl.splits > 0x7FFFFFFFl) {
+    const bool fold = causal && Tq == Tk;
+    const int steps = fold ? (Tq + 15) / 16 : (Tq + 7) / 8;
+    if (splits > steps) splits = steps;
+    const int slots = splits * launches;
+    if (planes * splits > 0x7FFFFFFFl) {
         DP_SET_ERR(ctx, "B * H = %ld is too large for one launch", planes);
         return DP_ERR_SHAPE;
     }
@@ -307,24 +362,37 @@ dp_status dpk_relbias_grads(dp_ctx* ctx, int n_layers, const void* const* dS, dp
         return DP_ERR_WORKSPACE;
     }
     float* part = slots > 1 ? (float*)ctx->ws : grads;
-    const size_t lds = (2 * SUMS * 256 + (size_t)(Tq + Tk - 1)) * sizeof(float);
+    // A band's distances: 8 b - 7 - off to 8 b + 7 - off.  Near are those that do not all lie from the last start on (without buckets of their own,
+    // behind the query).
+    const long off = Tk - Tq, last = starts[n - 1], behind = both && last > 1 ? last : 1;
+    const long lo = (off - last - 7 >= 0 ? (off - last - 7) / 8 : -((last + 7 - off + 7) / 8)) + 1, hi = (behind + 7 + off + 7) / 8 - 1;
+    const long rows = (Tq + 7) / 8, cols = (Tk + 7) / 8;
+    const int near_lo = (int)(lo > -rows ? lo : -rows), near_hi = (int)(hi < cols ? hi : cols);
+    const long d_lo = 8 * near_lo - 7 > 1 - Tq ? 8 * near_lo - 7 : 1 - Tq, d_hi = 8 * near_hi + 7 < Tk - 1 ? 8 * near_hi + 7 : Tk - 1;
+    // a wave where it has a block for every lane at most (6 layers x 256 x 16 x 20 x 20: 18 us, four waves 28)
+    const int threads = cols * steps <= 64 ? 64 : 256;
+    const size_t lds = (2 * SUMS * threads + (size_t)(d_hi >= d_lo ? d_hi - d_lo + 1 : 0)) * sizeof(float);
     for (int l0 = 0; l0 < n_layers; l0 += REL_LAYERS) {
         RelLayers t{};
         t.n = n_layers - l0 < REL_LAYERS ? n_layers - l0 : REL_LAYERS;
         for (int l = 0; l < t.n; ++l) t.x[l] = dS[l0 + l];
-        const dim3 grid((unsigned)(planes * pl.splits));
-        const int slot0 = l0 / REL_LAYERS * pl.splits;
+        const dim3 grid((unsigned)(planes * splits));
+        const int slot0 = l0 / REL_LAYERS * splits;
         auto launch = [&](auto kernel) {
             if (lds > 65536) DP_HIP_CHECK(ctx, hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024));
-            hipLaunchKernelGGL(kernel, grid, dim3(256), lds, ctx->stream, t, bk, lengths, causal, pl, B, H, Tq, Tk, part, slot0);
+            hipLaunchKernelGGL(kernel, grid, dim3(threads), lds, ctx->stream, t, bk, lengths, causal, splits, near_lo, near_hi, B, H, Tq, Tk, part, slot0);
             return DP_OK;
         };
-        const dp_status st = dt == DP_BF16 ? launch(relbias_grads_kernel<true>) : launch(relbias_grads_kernel<false>);
+        dp_status st;
+        if (dt == DP_BF16 && fold) st = threads == 64 ? launch(relbias_grads_kernel<true, true, 64>) : launch(relbias_grads_kernel<true, true, 256>);
+        else if (dt == DP_BF16) st = threads == 64 ? launch(relbias_grads_kernel<true, false, 64>) : launch(relbias_grads_kernel<true, false, 256>);
+        else if (fold) st = threads == 64 ? launch(relbias_grads_kernel<false, true, 64>) : launch(relbias_grads_kernel<false, true, 256>);
+        else st = threads == 64 ? launch(relbias_grads_kernel<false, false, 64>) : launch(relbias_grads_kernel<false, false, 256>);
         if (st != DP_OK) return st;
         DP_LAUNCH_CHECK(ctx, "relbias_grads");
     }
     if (slots > 1) {
-        const size_t blocks = (out + 255) / 256;
+        const size_t blocks = (out + 15) / 16;
         if (blocks > 0x7FFFFFFF) {
             DP_SET_ERR(ctx, "B * H * buckets too large for one launch");
             return DP_ERR_SHAPE;
