@@ -13,9 +13,27 @@ def _elements(shape):
     return n
 
 
+# Layers whose per-example gradients exist as tensors: the caller's own, or small ones that pass 1 writes.
+_HELD = ("grads", "relative_bias", "qk_norm")
+
+
+def _examples(layer):
+    kind = layer["kind"]
+    t = layer["grads"][0] if kind == "grads" else layer["dS"][0] if kind == "relative_bias" else layer["q"] if kind == "qk_norm" else layer["G"]
+    return t.shape[0]
+
+
 class StepRunner:
     """Owns the flat fp32 state (theta, m, v, clip-weighted sum S) of a manifest and the per-example
-    squared-norm buffer.  Tensors of the flat space follow the manifest order (LayerSpec.tensors())."""
+    squared-norm buffer.  Tensors of the flat space follow the manifest order (LayerSpec.tensors()).
+
+    A micro-batch is a list of one dict per layer of the manifest, `kind` and what the library's call for it reads: "dense" (A, G, has_bias),
+    "layernorm" (X, G), "embedding" (ids, G, V, distinct), "tied_embedding" (ids, G, H, dL), and
+      "grads"          grads: a list of tensors [B, ...], the examples' gradients of the layer's tensors, as the caller's backward holds them
+      "relative_bias"  dS: the list of score gradients of the layers that share the table, starts, bidirectional; lengths, causal if there are any
+      "qk_norm"        q, k, gain_q, gain_k, cos, sin, dyq, dyk; positions, interleaved, eps, and dq, dk to be written, if there are any
+    (the tensors of "relative_bias" are the table, those of "qk_norm" the two gains).  pass2 uses the gradients of the last two that pass1 of the
+    same micro-batch has left."""
 
     def __init__(self, ctx, manifest, max_batch, device="cuda:0"):
         import torch
@@ -45,6 +63,8 @@ class StepRunner:
         self.device = device
         self.ln_keep = {}
         self._kept_for = None
+        self.grad_keep = {}     # ... and the gradients of bias tables and of gains of queries and keys
+        self._grads_of = None   # examples whose gradients these are
 
     def view(self, buf, layer, k):
         off, shp = self.offsets[layer][k]
@@ -59,6 +79,78 @@ class StepRunner:
             buf = torch.empty(self.max_batch * 2 * d, dtype=torch.float32, device=self.device)
             self.ln_keep[k] = buf
         return buf
+
+    def _grad_buffer(self, k, shape):
+        """[examples, ...] floats for layer k of the manifest, of a buffer for max_batch examples that is allocated on first use."""
+        import torch
+
+        n = _elements(shape[1:])
+        buf = self.grad_keep.get(k)
+        if buf is None or buf.numel() < self.max_batch * n:
+            buf = self.grad_keep[k] = torch.empty(self.max_batch * n, dtype=torch.float32, device=self.device)
+        return buf[:shape[0] * n].view(*shape)
+
+    def _held_pass1(self, layers, held, nB, n):
+        """Gradients of the bias tables and gains, and the norms of all gradients that exist as tensors."""
+        self._grads_of = self._kept_for = None
+        if any(_examples(l) != nB for l in layers):
+            raise ValueError("layers of one micro-batch have as many examples each")
+        groups = self._held_tensors(layers, held, nB)
+        for k in held:
+            l = layers[k]
+            if l["kind"] == "relative_bias":
+                buckets = len(l["starts"]) * (2 if l["bidirectional"] else 1)
+                self.ctx.relative_bias_grads(l["dS"], l["starts"], l["bidirectional"], self._grad_buffer(k, (nB, buckets, l["dS"][0].shape[1])),
+                                             lengths=l.get("lengths"), causal=l.get("causal", False))
+            elif l["kind"] == "qk_norm":
+                self.ctx.qk_norm_grads(l["q"], l["k"], l["gain_q"], l["gain_k"], l["cos"], l["sin"], l["dyq"], l["dyk"],
+                                       self._grad_buffer(k, (nB, 2, l["q"].shape[3])), l.get("dq"), l.get("dk"), positions=l.get("positions"),
+                                       interleaved=l.get("interleaved", False), eps=l.get("eps", 1e-6))
+        self._grads_of = nB
+        for Xs, _ in groups:
+            self.ctx.sqnorms_grads(Xs, n)
+
+    def _held_pass2(self, layers, held, nB, C, n):
+        if self._grads_of != nB and any(layers[k]["kind"] != "grads" for k in held):
+            raise ValueError("pass1 of this micro-batch first: it leaves the gradients that are summed here")
+        for Xs, sums in self._held_tensors(layers, held, nB):
+            self.ctx.clip_accumulate_grads(Xs, C, n, sums)
+
+    def _held_tensors(self, layers, held, nB):
+        """[(gradients, their sums)] of one type each."""
+        by_type = {}
+        for k in held:
+            l = layers[k]
+            if l["kind"] == "grads":
+                if len(l["grads"]) != len(self.offsets[k]):
+                    raise ValueError(f"layer {k}: {len(l['grads'])} gradients for {len(self.offsets[k])} tensors")
+                pairs = [(g, self.view(self.S, k, j)) for j, g in enumerate(l["grads"])]
+            elif l["kind"] == "relative_bias":
+                n = len(l["starts"]) * (2 if l["bidirectional"] else 1)
+                pairs = [(self._grad_buffer(k, (nB, n, l["dS"][0].shape[1])), self.view(self.S, k, 0))]
+            else:   # the gains' sums lie next to each other: heads are a multiple of 8 wide, tensors start at multiples of 4 floats
+                off, d = self.offsets[k][0][0], l["q"].shape[3]
+                if [shp for _, shp in self.offsets[k]] != [(d,), (d,)]:
+                    raise ValueError(f"layer {k}: gains of shape ({d},) expected")
+                pairs = [(self._grad_buffer(k, (nB, 2, d)), self.S[off:off + 2 * d])]
+            for g, out in pairs:
+                if g.shape[0] != nB:
+                    raise ValueError(f"layer {k}: gradients of {g.shape[0]} examples in a micro-batch of {nB}")
+                if g.numel() != nB * out.numel():
+                    raise ValueError(f"layer {k}: gradients of shape {tuple(g.shape[1:])}, which is not that of the manifest's tensor")
+                xs, sums = by_type.setdefault(g.dtype, ([], []))
+                xs.append(g)
+                sums.append(out)
+        return by_type.values()
+
+    @staticmethod
+    def _split(layers):
+        """(the layers whose gradients never exist, their places, the places of the others)."""
+        held = [k for k, l in enumerate(layers) if l["kind"] in _HELD]
+        if not held:
+            return layers, range(len(layers)), held
+        rest = [k for k in range(len(layers)) if layers[k]["kind"] not in _HELD]
+        return [layers[k] for k in rest], rest, held
 
     @staticmethod
     def _ln_token(layers, nB):
@@ -75,7 +167,7 @@ class StepRunner:
 
     def _norms(self, layers):
         """(B, the norms of a micro-batch of B examples).  Refuses more examples than there are norms, and kept LayerNorm gradients, for."""
-        nB, most = layers[0]["G"].shape[0], min(self.max_batch, self.sqnorms.shape[0])
+        nB, most = _examples(layers[0]), min(self.max_batch, self.sqnorms.shape[0])
         if nB > most:
             raise ValueError(f"a micro-batch of {nB} examples: the buffers hold {most}")
         return nB, self.sqnorms[:nB]
@@ -93,6 +185,12 @@ class StepRunner:
         ctx = self.ctx
         nB, n = self._norms(layers)
         ctx.zero_f32(n)
+        layers_all = layers
+        layers, _, held = self._split(layers)
+        if held:
+            self._held_pass1(layers_all, held, nB, n)
+            if not layers:
+                return n
         if batch_dense and path == B_.DP_PATH_AUTO and type(ctx) is B_.Context:
             # the walk below in C++ (None: something it does not expect, nothing has been called)
             done = B_._native.pass1(ctx.handle, layers, n, self.ln_keep, self._keep_buffer, self.max_batch)
@@ -158,11 +256,19 @@ class StepRunner:
         layers are independent, so dense layers of one shape are handed over together (the library cuts them into launches that fill the chip)."""
         ctx = self.ctx
         nB, n = self._norms(layers)
+        layers_all = layers
+        layers, places, held = self._split(layers)
         S = B_._f32(self.S)
         if self.S.numel() < self.P or not self.S.is_contiguous():
             raise ValueError("S must be a contiguous buffer of all parameters")
+        spans = self._spans
+        if held:
+            self._held_pass2(layers_all, held, nB, C, n)
+            if not layers:
+                return
+            spans = [self._spans[k] for k in places]
         if batch_dense and type(ctx) is B_.Context:
-            done = B_._native.pass2(ctx.handle, layers, C, n, self.S, self._spans, self.ln_keep, self._kept_for, self.max_batch)
+            done = B_._native.pass2(ctx.handle, layers, C, n, self.S, spans, self.ln_keep, self._kept_for, self.max_batch)
             if done is not None:
                 if type(done) is tuple:
                     B_._check(ctx.handle, *done)
@@ -174,26 +280,26 @@ class StepRunner:
             if kind == "dense":
                 A, G = l["A"], l["G"]
                 if batch_dense:
-                    at = self._at[k]
+                    at = self._at[places[k]]
                     groups.setdefault((A.shape, G.shape, A.dtype), []).append(
                         (A.data_ptr(), G.data_ptr(), S + at[0], S + at[1] if l["has_bias"] else None))
                 else:
-                    sb = self.view(self.S, k, 1) if l["has_bias"] else None
-                    ctx.clip_accumulate_dense(A, G, C, n, self.view(self.S, k, 0), sb)
+                    sb = self.view(self.S, places[k], 1) if l["has_bias"] else None
+                    ctx.clip_accumulate_dense(A, G, C, n, self.view(self.S, places[k], 0), sb)
             elif kind == "layernorm":
                 if batch_dense:
                     ln_groups.setdefault((l["X"].shape, l["X"].dtype), []).append(k)
                 else:
-                    ctx.clip_accumulate_layernorm(l["X"], l["G"], C, n, self.view(self.S, k, 0), self.view(self.S, k, 1))
+                    ctx.clip_accumulate_layernorm(l["X"], l["G"], C, n, self.view(self.S, places[k], 0), self.view(self.S, places[k], 1))
             elif kind == "tied_embedding":
-                ctx.clip_accumulate_tied_embedding(l["ids"], l["G"], l["H"], l["dL"], C, n, self.view(self.S, k, 0))
+                ctx.clip_accumulate_tied_embedding(l["ids"], l["G"], l["H"], l["dL"], C, n, self.view(self.S, places[k], 0))
             elif l.get("distinct"):
-                ctx.clip_accumulate_positions(l["G"], C, n, self.view(self.S, k, 0))   # position ids: no sort needed
+                ctx.clip_accumulate_positions(l["G"], C, n, self.view(self.S, places[k], 0))   # position ids: no sort needed
             else:
-                ctx.clip_accumulate_embedding(l["ids"], l["G"], l["V"], C, n, self.view(self.S, k, 0))
+                ctx.clip_accumulate_embedding(l["ids"], l["G"], l["V"], C, n, self.view(self.S, places[k], 0))
         kept = self._kept_for is not None and self._kept_for == self._ln_token(layers, nB)   # pass 1 of this very micro-batch left the LayerNorm gradients behind
         for sel in ln_groups.values():
-            sg, sb = [S + self._at[k][0] for k in sel], [S + self._at[k][1] for k in sel]
+            sg, sb = [S + self._at[places[k]][0] for k in sel], [S + self._at[places[k]][1] for k in sel]
             if kept:
                 d = layers[sel[0]]["X"].shape[-1]
                 ctx.clip_accumulate_layernorm_kept([self.ln_keep[k] for k in sel], nB, d, C, n, sg, sb)
