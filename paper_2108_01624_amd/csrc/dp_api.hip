@@ -86,9 +86,11 @@ dp_status dp_create(dp_ctx** out, void* hip_stream, size_t workspace_bytes) {
     float* static_scratch = nullptr;  // looked up here so that dp_noise_adamw_snr_static finds it ready on this device
     if (e == hipSuccess && dpk_static_scratch(&static_scratch) != DP_OK) e = hipErrorInvalidSymbol;
     if (e == hipSuccess) e = hipMalloc((void**)&ctx->ws, ctx->ws_bytes);
-    if (e == hipSuccess) e = hipMalloc((void**)&ctx->err_word, sizeof(int));
+    constexpr size_t WORDS = 256;  // the error word and, in a line of its own, the ticket
+    if (e == hipSuccess) e = hipMalloc((void**)&ctx->err_word, WORDS);
     if (e == hipSuccess) e = hipMalloc((void**)&ctx->cbuf, (size_t)ctx->cbuf_cap * sizeof(float));
-    if (e == hipSuccess) e = hipMemset(ctx->err_word, 0, sizeof(int));
+    if (e == hipSuccess) e = hipMemset(ctx->err_word, 0, WORDS);
+    if (e == hipSuccess) ctx->ticket = (uint32_t*)ctx->err_word + 32;
     if (e != hipSuccess) {
         if (ctx->ws) (void)hipFree(ctx->ws);
         if (ctx->err_word) (void)hipFree(ctx->err_word);

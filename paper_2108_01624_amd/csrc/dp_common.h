@@ -21,6 +21,7 @@ struct dp_ctx {
     char* ws;         // device workspace
     size_t ws_bytes;
     int* err_word;    // device: bit 0 = token id out of range, bit 1 = a squared norm that is not a finite number
+    uint32_t* ticket; // device: 0 between calls; workgroups of a launch count themselves here, the last one sets it back
     float* cbuf;      // device: clip factors of the current micro-batch
     int cbuf_cap;     // capacity of cbuf in floats
     int prof_on;

@@ -12,6 +12,8 @@ constexpr int HELD_TABLE = 160;          // tensors per launch: their table is a
 constexpr uint64_t HELD_ENTRY = 1ull << 31;  // most elements of an entry of one unit; longer tensors are several entries
 constexpr uint64_t HELD_PIECE = 16384;   // elements of a workgroup of the norms and of the scaled gradients
 constexpr int WAVE_ROW = 4096;           // rows up to this length are one wave's
+constexpr unsigned ADD_GRID = 256;       // most workgroups, and units, of a launch of norms whose last workgroup adds them up
+constexpr int ADD_UNITS = 16;
 constexpr int ADD_COLS = 256 * 4;        // columns of a workgroup of the sums, one unit
 constexpr int SUM_COLS = 64 * 8;         // ... several units
 constexpr uint64_t LAST_LEVEL = 192ull << 20;  // bytes of the 256 MiB behind the L2s that a gradient may count on
@@ -131,10 +133,13 @@ __device__ __forceinline__ HeldPiece held_piece(uint32_t count, uint32_t k, int 
 }
 
 // part[unit * J + y[l] + piece] = sum of squares.  Four independent chains a thread, four loads in flight.
-template <bool BF16, bool STREAM>
-__global__ __launch_bounds__(256) void held_sqnorms_kernel(HeldTable t, int B, uint32_t per, uint32_t J, float* __restrict__ part) {
+// ADD: a launch of few workgroups, the only one; the last of them adds the parts to the norms (a launch behind it would cost as much again).
+template <bool BF16, bool STREAM, bool ADD>
+__global__ __launch_bounds__(256) void held_sqnorms_kernel(HeldTable t, int B, uint32_t per, uint32_t J, float* __restrict__ part, float* __restrict__ sqnorms,
+                                                           uint32_t* __restrict__ ticket) {
     typedef Held<BF16, STREAM> IO;
     __shared__ float red[4];
+    __shared__ bool last;
     const int l = held_tensor(t, blockIdx.x);
     const uint32_t count = t.count[l];
     const HeldPiece p = held_piece(count, blockIdx.x - t.first[l], B, per);
@@ -169,6 +174,21 @@ __global__ __launch_bounds__(256) void held_sqnorms_kernel(HeldTable t, int B, u
     } else {
         sum = dp_block_sum<256>(sum, red);
         if (threadIdx.x == 0) *out = sum;
+    }
+    if constexpr (ADD) {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");  // every thread's own part
+        __syncthreads();
+        if (threadIdx.x == 0) last = __hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
+        __syncthreads();
+        if (!last) return;
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+        for (int i = threadIdx.x >> 6; i < B; i += 4) {
+            float s = 0.f;
+            for (uint32_t j = threadIdx.x & 63; j < J; j += 64) s += __hip_atomic_load(part + (size_t)i * J + j, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            s = dp_wave_sum(s);
+            if ((threadIdx.x & 63) == 0) sqnorms[i] += s;
+        }
+        if (threadIdx.x == 0) __hip_atomic_store(ticket, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
 }
 
@@ -403,20 +423,26 @@ dp_status dpk_held_sqnorms(dp_ctx* ctx, int n, const void* const* X, const uint6
         const uint32_t width = (uint32_t)J;
         auto blocks = [&](uint64_t c) { return held_blocks(c, per, B); };
         auto columns = [&](uint64_t c) { return held_columns(c, per, B); };
+        bool added = false;
         const dp_status st = held_launches(ctx, m, X + l0, nullptr, count + l0, B, size, 4, false, blocks, columns, [&](const HeldTable& t, unsigned grid) {
-            auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, ctx->stream, t, B, per, width, part); };
-            if (dt == DP_BF16 && stream) launch(held_sqnorms_kernel<true, true>);
-            else if (dt == DP_BF16) launch(held_sqnorms_kernel<true, false>);
-            else if (stream) launch(held_sqnorms_kernel<false, true>);
-            else launch(held_sqnorms_kernel<false, false>);
+            uint64_t cols = 0;
+            for (int l = 0; l < t.n; ++l) cols += held_columns(t.count[l], per, B);
+            added = cols == width && grid <= ADD_GRID && B <= ADD_UNITS;
+            auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, ctx->stream, t, B, per, width, part, sqnorms, ctx->ticket); };
+            if (dt == DP_BF16 && added) launch(held_sqnorms_kernel<true, false, true>);
+            else if (added) launch(held_sqnorms_kernel<false, false, true>);
+            else if (dt == DP_BF16 && stream) launch(held_sqnorms_kernel<true, true, false>);
+            else if (dt == DP_BF16) launch(held_sqnorms_kernel<true, false, false>);
+            else if (stream) launch(held_sqnorms_kernel<false, true, false>);
+            else launch(held_sqnorms_kernel<false, false, false>);
             DP_LAUNCH_CHECK(ctx, "held_sqnorms");
             return DP_OK;
         });
         if (st != DP_OK) return st;
-        if (width > 512) {
+        if (width > 512 && !added) {
             hipLaunchKernelGGL(held_finish_kernel, dim3(B), dim3(1024), 0, ctx->stream, part, width, sqnorms);
             DP_LAUNCH_CHECK(ctx, "held_finish");
-        } else if (width > 0) {
+        } else if (width > 0 && !added) {
             const dp_status fin = dpk_finish_partials(ctx, part, B, (int)width, sqnorms);
             if (fin != DP_OK) return fin;
         }

@@ -26,12 +26,14 @@ struct Buckets {
 // The bucket of a key `rel` behind its query (negative: in front), by a side's n starts.
 __device__ __forceinline__ int bucket_of(const int* start, int n, int both, int rel) {
     const int dist = rel <= 0 ? -rel : both ? rel : 0;
-    int lo = 0, hi = n;  // the last start that is not above the distance
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (start[mid] <= dist) lo = mid;
-        else hi = mid;
-    }
+    int lo = 0, hi = n;  // the last start that is not above the distance: of most places of a long line the last of all
+    if (dist >= start[n - 1]) lo = n - 1;
+    else
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (start[mid] <= dist) lo = mid;
+            else hi = mid;
+        }
     return both && rel > 0 ? lo + n : lo;
 }
 
