@@ -16,8 +16,9 @@
  * then pass 2 (dp_clip_accumulate_* over every layer, "+=" into the fp32 sum buffers), and after the
  * last micro-batch one dp_noise_adamw over the flat parameter space.
  *
- * Per-example gradients of the weight tensors are never materialised (the one exception is optional and small:
- * dp_sqnorms_layernorm_keep writes the 2 d numbers of a LayerNorm per example).  For a dense layer y = xW + b with inputs A_i [T, d_in]
+ * Per-example gradients of the weight tensors are never materialised (the exceptions are small: dp_sqnorms_layernorm_keep writes the
+ * 2 d numbers of a LayerNorm per example, dp_relative_bias_grads those of a bias table, dp_qk_norm_grads those of two gains; what the caller
+ * itself holds goes to dp_sqnorms_grads and dp_clip_accumulate_grads).  For a dense layer y = xW + b with inputs A_i [T, d_in]
  * and output gradients G_i [T, d_out] of example i (the outer-product form of the fully connected
  * layer's gradient, Section 4.3) the example's weight gradient is A_i^T G_i and its bias gradient is
  * sum_t G_i[t, :].
@@ -240,7 +241,7 @@ dp_status dp_clip_factors(dp_ctx* ctx, const float* sqnorms, int B, float C, flo
  * dp_relative_bias_grads and dp_qk_norm_grads write) or, with B = 1, the whole gradient of one unit that is clipped as such (a user, a
  * micro-batch).  The norms add to those of the other calls of pass 1.  X and counts are HOST arrays, read during the call only; pointers
  * need the alignment of an element only, counts any value; tensors of no elements are passed over, their pointer is not looked at.
- * Tensors of different types go into calls of their own.  Up to 160 tensors share a launch.  With B > 1 counts end at 2^32 - 16 (DP_ERR_SHAPE above).
+ * Tensors of different types go into calls of their own.  Up to 160 tensors share a launch.  With B > 1 counts end at 2^31 (DP_ERR_SHAPE above).
  * ------------------------------------------------------------------------------------------------- */
 
 /* sqnorms[i] += sum_l sum_k X[l][i, k]^2.  The norms of a tensor's pieces pass through the workspace (a float per unit for every tensor,

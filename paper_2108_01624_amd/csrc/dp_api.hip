@@ -454,7 +454,7 @@ static dp_status check_grads(dp_ctx* ctx, int n, const void* const* X, const uin
     const uintptr_t low = dtype == DP_BF16 ? 1 : 3;
     for (int l = 0; l < n; ++l) {
         if (counts[l] == 0) continue;
-        if (counts[l] > (1ull << 59) / (uint64_t)B) FAIL(ctx, DP_ERR_SHAPE, "counts[%d] is too large", l);
+        if (counts[l] > (B > 1 ? 1ull << 31 : 1ull << 59)) FAIL(ctx, DP_ERR_SHAPE, "counts[%d] is too large", l);
         if (!X[l]) FAIL(ctx, DP_ERR_NULL, "X[%d] is NULL", l);
         if ((uintptr_t)X[l] & low) FAIL(ctx, DP_ERR_ALIGN, "X[%d] is not aligned to its elements", l);
         if (!out) continue;

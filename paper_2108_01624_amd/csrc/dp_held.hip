@@ -9,7 +9,7 @@
 namespace {
 
 constexpr int HELD_TABLE = 160;          // tensors per launch: their table is a kernel argument, of less than 4 KiB
-constexpr uint64_t HELD_ENTRY = 1ull << 31;  // most elements of an entry of one unit; longer tensors are several entries
+constexpr uint64_t HELD_ENTRY = 1ull << 31;  // most elements of an entry (32-bit counters have room behind them); one unit's longer tensors are several entries
 constexpr uint64_t HELD_PIECE = 16384;   // elements of a workgroup of the norms and of the scaled gradients
 constexpr int WAVE_ROW = 4096;           // rows up to this length are one wave's
 constexpr unsigned ADD_GRID = 256;       // most workgroups, and units, of a launch of norms whose last workgroup adds them up
@@ -341,10 +341,6 @@ dp_status held_launches(dp_ctx* ctx, int n, const void* const* X, void* const* Y
         return st;
     };
     for (int l = 0; l < n; ++l) {
-        if (B > 1 && count[l] > 0xFFFFFFF0ull) {
-            DP_SET_ERR(ctx, "tensor %d: more than 2^32 - 16 elements of a unit", l);
-            return DP_ERR_SHAPE;
-        }
         for (uint64_t done = 0; done < count[l];) {
             const uint64_t c = B > 1 || count[l] - done <= HELD_ENTRY ? count[l] - done : HELD_ENTRY;
             const uintptr_t x = (uintptr_t)X[l] + done * xsize, y = Y ? (uintptr_t)Y[l] + done * ysize : 0;

@@ -128,7 +128,7 @@ struct Place {
         const int s = lane / LPH;
         token = 0;
         head = s;
-        if (S.tpw > 1) {
+        if (S.tpw > 1 && S.H) {
             token = s / S.H;
             head = s - token * S.H;
         }

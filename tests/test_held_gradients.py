@@ -187,7 +187,7 @@ def test_refusals():
     assert norms(n=0) == 0 and norms(B=0) == 0
     assert norms(dt=2) == -3 and norms(n=-1) == -2 and norms(B=-1) == -2 and norms(sq=None) == -1 and norms(sq=p + 2) == -4
     assert norms(X=None) == -1 and norms(c=None) == -1 and norms(X=tab(None)) == -1 and norms(X=tab(p + 2)) == -4 and norms(X=tab(p + 1), dt=H) == -4
-    assert norms(c=cnt(1 << 60)) == -2
+    assert norms(c=cnt(1 << 60)) == -2 and norms(c=cnt((1 << 31) + 1), B=2) == -2
     sums = lambda n=1, X=tab(p), c=cnt(4), dt=F, B=1, C=1.0, sq=p, S=tab(p): lib.dp_clip_accumulate_grads(ctx, n, X, c, dt, B, C, sq, S)
     assert sums(S=None) == -1 and sums(S=tab(None)) == -1 and sums(S=tab(p + 2)) == -4 and sums(C=0.0) == -5 and sums(C=float("nan")) == -5
     assert sums(dt=H, S=tab(p + 2)) == -4 and sums(B=0) == 0 and sums(n=0) == 0 and sums(n=0, S=None, X=None, c=None) == 0
