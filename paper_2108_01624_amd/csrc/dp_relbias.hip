@@ -94,16 +94,23 @@ struct RelLayers {
 // of blocks; gr such groups take the steps (rows of blocks, pairs of them under FOLD) in turn, `m` each, and gl of these the layers in turn.
 struct RelPlan {
     int nb, np, steps;  // blocks in a row, threads for one (of which there may be more than `wide`), steps
-    int per;            // steps of a workgroup
+    int used, per;      // workgroups that share the steps, and steps of each
     int wide, gr, gl, m;
 };
+// rows, cols: what counts of a plane that has up to splits workgroups for all_rows x all_cols; a short example has fewer to itself, by its share of
+// the places.
 template <bool FOLD, int NT>
-__device__ __forceinline__ RelPlan rel_plan(int layers, int rows, int cols, int splits) {
+__device__ __forceinline__ RelPlan rel_plan(int layers, int rows, int cols, int all_rows, int all_cols, int splits) {
     RelPlan p;
     p.nb = max((cols + 7) / 8, 1);
     p.np = FOLD ? p.nb + 1 : p.nb;
     p.steps = FOLD ? (p.nb + 1) / 2 : (rows + 7) / 8;
-    p.per = max((int)((unsigned)(p.steps + splits - 1) / (unsigned)splits), 1);
+    p.used = splits;
+    if (splits > 1 && cols < all_cols) {
+        const float share = (float)rows * (float)cols / ((float)all_rows * (float)all_cols);
+        p.used = min(max((int)ceilf(share * (float)splits), 1), splits);
+    }
+    p.per = max((int)((unsigned)(p.steps + p.used - 1) / (unsigned)p.used), 1);
     p.wide = min(p.np, NT);
     const unsigned groups = (unsigned)NT / (unsigned)p.wide;
     p.m = (unsigned)(p.per + groups - 1) / groups;
@@ -143,7 +150,12 @@ __global__ __launch_bounds__(NT) void relbias_grads_kernel(RelLayers t, Buckets 
     int len = Tk;
     if (lengths) len = min(max(lengths[i], 0), Tk);
     const int nq = min(max(len - off, 0), Tq);  // rows and columns that count: nq and len
-    const RelPlan pl = rel_plan<FOLD, NT>(t.n, nq, len, splits);
+    const RelPlan pl = rel_plan<FOLD, NT>(t.n, nq, len, Tq, Tk, splits);
+    if (s >= pl.used) {
+        const int nbk = bk.both ? 2 * bk.n : bk.n;
+        for (int j = tid; j < nbk; j += NT) part[(((size_t)(slot0 + s) * B + i) * nbk + j) * H + h] = 0.f;
+        return;
+    }
     const int s0 = s * pl.per, s1 = min(s0 + pl.per, pl.steps);
     const int grp = tid / (unsigned)pl.wide, pp = tid - grp * pl.wide, lg = grp / (unsigned)pl.gr, rg = grp - lg * pl.gr;
     const bool works = lg < pl.gl;
@@ -202,7 +214,9 @@ __global__ __launch_bounds__(NT) void relbias_grads_kernel(RelLayers t, Buckets 
                 }
                 const int at = q0 * Tk + k0;
                 for (int l = lg; l < t.n; l += pl.gl) {
-                    const elem* x = (const elem*)t.x[l] + (size_t)mat * Tq * Tk + at;
+                    // (where the layers are not shared out, theirs is a scalar load)
+                    const void* base = pl.gl == 1 ? t.x[__builtin_amdgcn_readfirstlane(l)] : t.x[l];
+                    const elem* x = (const elem*)base + (size_t)mat * Tq * Tk + at;
                     uint32_t v[8][W];
 #pragma unroll
                     for (int r = 0; r < 8; ++r) {
@@ -347,8 +361,9 @@ dp_status dpk_relbias_grads(dp_ctx* ctx, int n_layers, const void* const* dS, dp
     const long planes = (long)B * H;
     const int launches = (n_layers + REL_LAYERS - 1) / REL_LAYERS;
     // workgroups of a plane: as many as fill the chip, four to a CU, as long as their parts fit (twice as many: 6 x 8 x 16 x 512 x 512 under a
-    // causal mask 46 us instead of 43, half as many 46)
-    int splits = planes >= 1024 ? 1 : (int)(1024 / planes);
+    // causal mask 46 us instead of 43, half as many 46); twice as many where examples may be shorter, and need fewer (6 layers of 24 x 12 of up to 509 tokens, causal: 101 -> 94 us)
+    const int aim = lengths ? 2048 : 1024;
+    int splits = planes >= aim ? 1 : (int)(aim / planes);
     const size_t room = ctx->ws_bytes / (out * sizeof(float));
     if ((size_t)splits * launches > room) splits = room / launches > 1 ? (int)(room / launches) : 1;
     const bool fold = causal && Tq == Tk;
