@@ -12,6 +12,7 @@
 namespace {
 
 constexpr int HELD_TABLE = 160;          // tensors per launch: their table is a kernel argument, of less than 4 KiB
+constexpr int HELD_FEW = 32;             // a small table where it is enough (16 tensors: a call of the sums 4.7 -> 3.8 us of host time)
 constexpr uint64_t HELD_ENTRY = 1ull << 31;  // most elements of an entry (32-bit counters have room behind them); one unit's longer tensors are several entries
 constexpr uint64_t HELD_PIECE = 16384;   // elements of a workgroup of the norms (334 M bf16: 98 us; 4,096: 101, 65,536: 102)
 constexpr int WAVE_ROW = 4096;           // rows up to this length are one wave's (256 units of 96 rows of 2,048 bf16: 45 us norms and sums; up to 1,024: 59)
@@ -83,17 +84,35 @@ struct Held {
 };
 
 // The tensors of a launch.  Workgroups first[l] .. first[l + 1] - 1 are tensor l's.
+template <int N>
 struct HeldTable {
-    const void* x[HELD_TABLE];   // (pointers, not numbers: the compiler takes those of an argument for global memory)
-    void* y[HELD_TABLE];         // sums or scaled gradients; norms: the first of the tensor's partial norms, as a number
-    uint32_t count[HELD_TABLE];  // elements of a unit
-    uint32_t first[HELD_TABLE];
+    const void* x[N];   // (pointers, not numbers: the compiler takes those of an argument for global memory)
+    void* y[N];         // sums or scaled gradients; norms: the first of the tensor's partial norms, as a number
+    uint32_t count[N];  // elements of a unit
+    uint32_t first[N];
     int n;
 };
+typedef HeldTable<HELD_TABLE> HeldFull;
+
+// launch(table): the full one, or a small copy of it.
+template <typename Launch>
+void with_table(const HeldFull& t, Launch launch) {
+    if (t.n > HELD_FEW) return launch(t);
+    HeldTable<HELD_FEW> few;
+    for (int l = 0; l < t.n; ++l) {
+        few.x[l] = t.x[l];
+        few.y[l] = t.y[l];
+        few.count[l] = t.count[l];
+        few.first[l] = t.first[l];
+    }
+    few.n = t.n;
+    launch(few);
+}
 
 // The tensor of workgroup b: a search by halves over scalar loads.  (Two entries a lane and ballots, one round of vector loads, cost a
 // workgroup of 1,024 columns more than its work: 334 M bf16 elements added to their sums 684 us that way, 503 this way.)
-__device__ __forceinline__ int held_tensor(const HeldTable& t, uint32_t b) {
+template <int N>
+__device__ __forceinline__ int held_tensor(const HeldTable<N>& t, uint32_t b) {
     int lo = 0, hi = t.n;
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
@@ -135,8 +154,8 @@ __device__ __forceinline__ HeldPiece held_piece(uint32_t count, uint32_t k, int 
 
 // part[unit * J + y[l] + piece] = sum of squares.  Four independent chains a thread, four loads in flight.
 // ADD: a launch of few workgroups, the only one; the last of them adds the parts to the norms (a launch behind it would cost as much again).
-template <bool BF16, bool STREAM, bool ADD>
-__global__ __launch_bounds__(256) void held_sqnorms_kernel(HeldTable t, int B, uint32_t per, uint32_t J, float* __restrict__ part, float* __restrict__ sqnorms,
+template <bool BF16, bool STREAM, bool ADD, int N>
+__global__ __launch_bounds__(256) void held_sqnorms_kernel(HeldTable<N> t, int B, uint32_t per, uint32_t J, float* __restrict__ part, float* __restrict__ sqnorms,
                                                            uint32_t* __restrict__ ticket) {
     typedef Held<BF16, STREAM> IO;
     __shared__ float red[4];
@@ -217,8 +236,8 @@ __device__ __forceinline__ float held_factor(const float* sqnorms, int i, float 
 
 // sums[k] += c x[k], one unit.  Four elements a thread, the sums' access the wide one, neighbouring workgroups on neighbouring
 // memory: 334 M bf16 elements 504 us (6.6 TB/s); eight elements a thread 604, two or four times four 548 and 565.
-template <bool BF16>
-__global__ __launch_bounds__(256) void held_add_kernel(HeldTable t, float C, const float* __restrict__ sqnorms, int* __restrict__ err) {
+template <bool BF16, int N>
+__global__ __launch_bounds__(256) void held_add_kernel(HeldTable<N> t, float C, const float* __restrict__ sqnorms, int* __restrict__ err) {
     typedef Held<BF16> IO;
     const int l = held_tensor(t, blockIdx.x);
     const uint32_t count = t.count[l], k = (blockIdx.x - t.first[l]) * ADD_COLS + threadIdx.x * 4;
@@ -241,8 +260,8 @@ __global__ __launch_bounds__(256) void held_add_kernel(HeldTable t, float C, con
 }
 
 // sums[k] += sum_i c_i x[i][k]: RG waves share the units of 512 columns, eight a lane, and are added in a fixed order.
-template <bool BF16, int RG>
-__global__ __launch_bounds__(64 * RG) void held_sums_kernel(HeldTable t, int B, float C, const float* __restrict__ sqnorms, int* __restrict__ err) {
+template <bool BF16, int RG, int N>
+__global__ __launch_bounds__(64 * RG) void held_sums_kernel(HeldTable<N> t, int B, float C, const float* __restrict__ sqnorms, int* __restrict__ err) {
     typedef Held<BF16> IO;
     __shared__ float fac[FACTORS];
     __shared__ float red[RG][SUM_COLS];
@@ -298,8 +317,8 @@ __global__ __launch_bounds__(64 * RG) void held_sums_kernel(HeldTable t, int B, 
 }
 
 // y[i][k] = c_i x[i][k], rounded once; nothing to do in place where c_i is one.
-template <bool BF16>
-__global__ __launch_bounds__(256) void held_scale_kernel(HeldTable t, int B, uint32_t per, float C, const float* __restrict__ sqnorms, int* __restrict__ err) {
+template <bool BF16, int N>
+__global__ __launch_bounds__(256) void held_scale_kernel(HeldTable<N> t, int B, uint32_t per, float C, const float* __restrict__ sqnorms, int* __restrict__ err) {
     typedef Held<BF16> IO;
     const int l = held_tensor(t, blockIdx.x);
     const uint32_t count = t.count[l];
@@ -330,7 +349,8 @@ bool held_overlap(uintptr_t a, uint64_t na, uintptr_t b, uint64_t nb) { return a
 template <typename Blocks, typename Columns, typename Go>
 dp_status held_launches(dp_ctx* ctx, int n, const void* const* X, void* const* Y, const uint64_t* count, int B, int xsize, int ysize, bool sums, Blocks blocks, Columns columns,
                         Go go) {
-    HeldTable t{};
+    HeldFull t;
+    t.n = 0;
     uint64_t grid = 0, col = 0;
     uintptr_t lo = UINTPTR_MAX, hi = 0;  // hull of the sums of a launch: in a flat buffer's order every tensor lies outside it
     auto flush = [&]() -> dp_status {
@@ -421,17 +441,20 @@ dp_status dpk_held_sqnorms(dp_ctx* ctx, int n, const void* const* X, const uint6
         auto blocks = [&](uint64_t c) { return held_blocks(c, per, B); };
         auto columns = [&](uint64_t c) { return held_columns(c, per, B); };
         bool added = false;
-        const dp_status st = held_launches(ctx, m, X + l0, nullptr, count + l0, B, size, 4, false, blocks, columns, [&](const HeldTable& t, unsigned grid) {
+        const dp_status st = held_launches(ctx, m, X + l0, nullptr, count + l0, B, size, 4, false, blocks, columns, [&](const HeldFull& full, unsigned grid) {
             uint64_t cols = 0;
-            for (int l = 0; l < t.n; ++l) cols += held_columns(t.count[l], per, B);
+            for (int l = 0; l < full.n; ++l) cols += held_columns(full.count[l], per, B);
             added = cols == width && grid <= ADD_GRID && B <= ADD_UNITS;
-            auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, ctx->stream, t, B, per, width, part, sqnorms, ctx->ticket); };
-            if (dt == DP_BF16 && added) launch(held_sqnorms_kernel<true, false, true>);
-            else if (added) launch(held_sqnorms_kernel<false, false, true>);
-            else if (dt == DP_BF16 && stream) launch(held_sqnorms_kernel<true, true, false>);
-            else if (dt == DP_BF16) launch(held_sqnorms_kernel<true, false, false>);
-            else if (stream) launch(held_sqnorms_kernel<false, true, false>);
-            else launch(held_sqnorms_kernel<false, false, false>);
+            with_table(full, [&](const auto& t) {
+                constexpr int N = sizeof(t.count) / sizeof(t.count[0]);
+                auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, ctx->stream, t, B, per, width, part, sqnorms, ctx->ticket); };
+                if (dt == DP_BF16 && added) launch(held_sqnorms_kernel<true, false, true, N>);
+                else if (added) launch(held_sqnorms_kernel<false, false, true, N>);
+                else if (dt == DP_BF16 && stream) launch(held_sqnorms_kernel<true, true, false, N>);
+                else if (dt == DP_BF16) launch(held_sqnorms_kernel<true, false, false, N>);
+                else if (stream) launch(held_sqnorms_kernel<false, true, false, N>);
+                else launch(held_sqnorms_kernel<false, false, false, N>);
+            });
             DP_LAUNCH_CHECK(ctx, "held_sqnorms");
             return DP_OK;
         });
@@ -457,14 +480,17 @@ dp_status dpk_held_sums(dp_ctx* ctx, int n, const void* const* X, const uint64_t
     // units would take 21.8 instead of 18.8.
     const bool tall = tiles < 256 && B >= 64;
     auto blocks = [&](uint64_t c) { return (c + cols - 1) / cols; };
-    return held_launches(ctx, n, X, (void* const*)sums, count, B, dt == DP_BF16 ? 2 : 4, 4, true, blocks, [](uint64_t) { return (uint64_t)0; }, [&](const HeldTable& t, unsigned grid) {
-        auto launch = [&](auto kernel, int threads, auto... args) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(threads), 0, ctx->stream, t, args..., C, sqnorms, ctx->err_word); };
-        if (B == 1 && dt == DP_BF16) launch(held_add_kernel<true>, 256);
-        else if (B == 1) launch(held_add_kernel<false>, 256);
-        else if (dt == DP_BF16 && tall) launch(held_sums_kernel<true, 16>, 1024, B);
-        else if (dt == DP_BF16) launch(held_sums_kernel<true, 4>, 256, B);
-        else if (tall) launch(held_sums_kernel<false, 16>, 1024, B);
-        else launch(held_sums_kernel<false, 4>, 256, B);
+    return held_launches(ctx, n, X, (void* const*)sums, count, B, dt == DP_BF16 ? 2 : 4, 4, true, blocks, [](uint64_t) { return (uint64_t)0; }, [&](const HeldFull& full, unsigned grid) {
+        with_table(full, [&](const auto& t) {
+            constexpr int N = sizeof(t.count) / sizeof(t.count[0]);
+            auto launch = [&](auto kernel, int threads, auto... args) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(threads), 0, ctx->stream, t, args..., C, sqnorms, ctx->err_word); };
+            if (B == 1 && dt == DP_BF16) launch(held_add_kernel<true, N>, 256);
+            else if (B == 1) launch(held_add_kernel<false, N>, 256);
+            else if (dt == DP_BF16 && tall) launch(held_sums_kernel<true, 16, N>, 1024, B);
+            else if (dt == DP_BF16) launch(held_sums_kernel<true, 4, N>, 256, B);
+            else if (tall) launch(held_sums_kernel<false, 16, N>, 1024, B);
+            else launch(held_sums_kernel<false, 4, N>, 256, B);
+        });
         DP_LAUNCH_CHECK(ctx, "held_sums");
         return DP_OK;
     });
@@ -474,9 +500,13 @@ dp_status dpk_held_scale(dp_ctx* ctx, int n, const void* const* X, const uint64_
     const uint32_t per = ADD_COLS;
     const int size = dt == DP_BF16 ? 2 : 4;
     auto blocks = [&](uint64_t c) { return held_blocks(c, per, B); };
-    return held_launches(ctx, n, X, Y, count, B, size, size, false, blocks, [](uint64_t) { return (uint64_t)0; }, [&](const HeldTable& t, unsigned grid) {
-        if (dt == DP_BF16) hipLaunchKernelGGL(held_scale_kernel<true>, dim3(grid), dim3(256), 0, ctx->stream, t, B, per, C, sqnorms, ctx->err_word);
-        else hipLaunchKernelGGL(held_scale_kernel<false>, dim3(grid), dim3(256), 0, ctx->stream, t, B, per, C, sqnorms, ctx->err_word);
+    return held_launches(ctx, n, X, Y, count, B, size, size, false, blocks, [](uint64_t) { return (uint64_t)0; }, [&](const HeldFull& full, unsigned grid) {
+        with_table(full, [&](const auto& t) {
+            constexpr int N = sizeof(t.count) / sizeof(t.count[0]);
+            auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), 0, ctx->stream, t, B, per, C, sqnorms, ctx->err_word); };
+            if (dt == DP_BF16) launch(held_scale_kernel<true, N>);
+            else launch(held_scale_kernel<false, N>);
+        });
         DP_LAUNCH_CHECK(ctx, "held_scale");
         return DP_OK;
     });
