@@ -491,27 +491,32 @@ dp_status dp_clip_grads(dp_ctx* ctx, int n_layers, const void* const* X, const u
     return dpk_held_scale(ctx, n_layers, X, counts, dtype, B, C, sqnorms, Y);
 }
 
-// d^m e^j < r^j e^m for whole numbers, n = m >= j, by comparing products of 32-bit words (at most 128 factors of 30 bits: 120 words).
+// d^m e^j < r^j e^m for whole numbers, by comparing products of 32-bit words (at most 128 factors of 30 bits: 120 words).
 static bool bucket_below(uint32_t d, uint32_t e, uint32_t r, int m, int j) {
-    uint32_t a[128] = {1}, b[128] = {1};
-    auto times = [](uint32_t* w, uint32_t f) {
-        uint64_t carry = 0;
-        for (int k = 0; k < 128; ++k) {
-            carry += (uint64_t)w[k] * f;
-            w[k] = (uint32_t)carry;
-            carry >>= 32;
+    struct Product {
+        uint32_t w[128] = {1};
+        int n = 1;  // words in use
+        void times(uint32_t f) {
+            uint64_t carry = 0;
+            for (int k = 0; k < n; ++k) {
+                carry += (uint64_t)w[k] * f;
+                w[k] = (uint32_t)carry;
+                carry >>= 32;
+            }
+            if (carry && n < 128) w[n++] = (uint32_t)carry;
         }
-    };
+    } a, b;
     for (int k = 0; k < m; ++k) {
-        times(a, d);
-        times(b, e);
+        a.times(d);
+        b.times(e);
     }
     for (int k = 0; k < j; ++k) {
-        times(a, e);
-        times(b, r);
+        a.times(e);
+        b.times(r);
     }
-    for (int k = 127; k >= 0; --k)
-        if (a[k] != b[k]) return a[k] < b[k];
+    if (a.n != b.n) return a.n < b.n;
+    for (int k = a.n - 1; k >= 0; --k)
+        if (a.w[k] != b.w[k]) return a.w[k] < b.w[k];
     return false;
 }
 
