@@ -5,7 +5,7 @@
 // entry of the sums; the scaled form reads and writes it.  Rows start wherever n_l puts them: wide accesses are declared with the
 // alignment of an element, which the hardware serves at any address.
 //
-// 334 M bf16 elements of 391 tensors, one unit: norms 109 us in three launches (6.1 TB/s), sums 556 us (6.0 TB/s of reading and writing);
+// 334 M bf16 elements of 388 tensors, one unit: norms 109 us in three launches (6.1 TB/s), sums 556 us (6.0 TB/s of reading and writing);
 // 128 units of 96 tensors of 8,192 bf16 elements: norms 34 us (6.0 TB/s), sums 42; 41 M fp32 elements scaled: 56 us (5.9 TB/s).
 #include "dp_common.h"
 
