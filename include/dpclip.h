@@ -294,7 +294,8 @@ dp_status dp_relative_bias_grads(dp_ctx* ctx, int n_layers, const void* const* d
  * dp_sync as DP_ERR_INDEX; its token's outputs are zero and it adds nothing to the gradients.
  *   q, k: [B, T, Hq, D] and [B, T, Hk, D] of `dtype`, a token's heads next to each other, tokens ldq / ldk numbers apart (at least Hq D / Hk D;
  *   more where they are parts of a fused projection's output).  Either may have no heads (its pointers are not looked at).  Element alignment.
- *   D in [8, 512] and R in [0, D], both multiples of 8; eps > 0.  No output overlaps an input (DP_ERR_VALUE).  Arithmetic in fp32.
+ *   D in [8, 512] and R in [0, D], both multiples of 8; eps a positive normal number; n_pos >= 1 if R > 0.  The range of memory that an
+ *   output lies in meets no input's (DP_ERR_VALUE).  Arithmetic in fp32.
  * ------------------------------------------------------------------------------------------------- */
 
 /* yq [B, T, Hq, D], yk [B, T, Hk, D], dense. */

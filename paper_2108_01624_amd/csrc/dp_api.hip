@@ -1,4 +1,5 @@
 // C ABI entry points: argument checks, context management and dispatch to the kernel launchers.
+#include <float.h>
 #include <limits.h>
 #include <math.h>
 #include <stdlib.h>
@@ -590,7 +591,7 @@ static dp_status check_qk(dp_ctx* ctx, const dp_qk_args& a) {
     if (a.Hq < 0 || a.Hk < 0 || (long)a.Hq + a.Hk > (1 << 20)) FAIL(ctx, DP_ERR_SHAPE, "Hq = %d, Hk = %d: 0 to 2^20 heads", a.Hq, a.Hk);
     if (a.D < 8 || a.D > 512 || a.D % 8) FAIL(ctx, DP_ERR_SHAPE, "D = %d: a multiple of 8 in [8, 512]", a.D);
     if (a.R < 0 || a.R > a.D || a.R % 8) FAIL(ctx, DP_ERR_SHAPE, "R = %d: a multiple of 8 in [0, D]", a.R);
-    if (!(a.eps > 0.f) || !isfinite(a.eps)) FAIL(ctx, DP_ERR_VALUE, "eps must be positive and finite");
+    if (!(a.eps >= FLT_MIN) || !isfinite(a.eps)) FAIL(ctx, DP_ERR_VALUE, "eps must be a positive normal number");
     const uintptr_t low = a.dtype == DP_BF16 ? 1 : 3;
     for (int s = 0; s < 2; ++s) {
         const int H = s ? a.Hk : a.Hq;

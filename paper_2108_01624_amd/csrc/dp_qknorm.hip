@@ -410,7 +410,7 @@ QkArgs make_args(dp_ctx* ctx, const dp_qk_args& a) {
     A.s[1].H = a.Hk;
     A.cos = a.cos;
     A.sin = a.sin;
-    A.pos = a.positions;
+    A.pos = a.R ? a.positions : nullptr;
     A.err = ctx->err_word;
     A.tokens = (long)a.B * a.T;
     A.n_pos = a.n_pos;

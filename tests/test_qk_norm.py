@@ -169,6 +169,19 @@ def test_positions_outside_the_table(dp, where):
 
 
 @pytest.mark.gpu
+def test_positions_are_not_looked_at_without_a_rotation(dp):
+    q, k, gq, gk, _, _, _, dyq, dyk = _make(2, 5, 3, 1, 40, 0, "bf16", "dense", 10)
+    out = []
+    for p in (None, torch.full((2, 5), -7, dtype=torch.int32, device=DEV)):
+        y = [torch.empty_like(q), torch.empty_like(k), torch.empty(2, 2, 40, device=DEV)]
+        dp.qk_norm(q, k, gq, gk, None, None, *y[:2], positions=p)
+        dp.qk_norm_grads(q, k, gq, gk, None, None, dyq, dyk, y[2], positions=p)
+        dp.sync()
+        out.append(y)
+    assert all(torch.equal(a, b) for a, b in zip(*out))
+
+
+@pytest.mark.gpu
 def test_zero_rows_and_no_tokens(dp):
     q, k, gq, gk, cos, sin, pos, dyq, dyk = _make(2, 3, 2, 2, 32, 32, "f32", "dense", 8)
     q[1, 1] = 0
@@ -223,6 +236,7 @@ def test_refusals():
         for kw in (dict(q=p + 2), dict(k=p + 1, dt=pkg.DP_BF16), dict(gq=p + 2), dict(cos=p + 2), dict(pos=p + 2)):
             assert call(**kw) == -4, kw
         assert call(dt=3) == -3 and call(eps=0.0) == -5 and call(eps=-1.0) == -5 and call(eps=float("inf")) == -5 and call(eps=float("nan")) == -5
+        assert call(eps=1e-39) == -5 and call(n_pos=0) == -2 and call(n_pos=0, B=0) == 0
     assert forward(Hq=0, Hk=0, q=None, k=None) == 0
     assert forward(yq=None) == -1 and forward(yk=None) == -1 and forward(yq=far + 2) == -4 and forward(yq=p) == -5 and forward(yk=p + 64) == -5
     assert back(dyq=None) == -1 and back(dyk=p + 2) == -4 and back(g=None) == -1 and back(dq=None) == -1 and back(dk=p) == -5 and back(dq=far + 1) == -4
