@@ -364,10 +364,19 @@ dp_status dpk_relbias_grads(dp_ctx* ctx, int n_layers, const void* const* dS, dp
     // causal mask 46 us instead of 43, half as many 46); twice as many where examples may be shorter, and need fewer (6 layers of 24 x 12 of up to 509 tokens, causal: 101 -> 94 us)
     const int aim = lengths ? 2048 : 1024;
     int splits = planes >= aim ? 1 : (int)(aim / planes);
-    const size_t room = ctx->ws_bytes / (out * sizeof(float));
-    if ((size_t)splits * launches > room) splits = room / launches > 1 ? (int)(room / launches) : 1;
     const bool fold = causal && Tq == Tk;
     const int steps = fold ? (Tq + 15) / 16 : (Tq + 7) / 8;
+    if (lengths) {
+        // Short examples leave the last workgroups of their planes empty.  Up to 8,192 where a thread then still has two of its plane's steps, so that
+        // the longest examples are not what all wait for (2 layers of 128 x 12 of up to 509 tokens, causal: 171 -> 155 us); and an odd number, so that
+        // the same part of a plane does not always come to the same XCD (2 layers of 16 x 16 x 1,024, causal: 128 us with 8, 112 with 9; 8 where
+        // 7 had been, 6 layers of 24 x 12 x 509: 160 -> 211.  Planes in the inner order, which any number allows: 104 us instead of 94 under its mask).
+        const long across = (Tk + 7) / 8 + (fold ? 1 : 0), chain = steps / (across < 256 ? 256 / across : 1);
+        const long more = chain / 2 < 8192 / planes ? chain / 2 : 8192 / planes;
+        splits = (more > splits ? (int)more : splits) | 1;
+    }
+    const size_t room = ctx->ws_bytes / (out * sizeof(float));
+    if ((size_t)splits * launches > room) splits = room / launches > 1 ? (int)(room / launches) : 1;
     if (splits > steps) splits = steps;
     const int slots = splits * launches;
     if (planes * splits > 0x7FFFFFFFl) {
