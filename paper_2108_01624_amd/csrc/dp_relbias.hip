@@ -405,7 +405,8 @@ dp_status dpk_relbias_grads(dp_ctx* ctx, int n_layers, const void* const* dS, dp
         const dim3 grid((unsigned)(planes * splits));
         const int slot0 = l0 / REL_LAYERS * splits;
         auto launch = [&](auto kernel) {
-            if (lds > 65536) DP_HIP_CHECK(ctx, hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024));
+            // (what this launch takes, 158 KiB at most: with the kernel's static words a request for all 160 KiB of a CU is refused)
+            if (lds > 65536) DP_HIP_CHECK(ctx, hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
             hipLaunchKernelGGL(kernel, grid, dim3(threads), lds, ctx->stream, t, bk, lengths, causal, splits, near_lo, near_hi, B, H, Tq, Tk, part, slot0);
             return DP_OK;
         };

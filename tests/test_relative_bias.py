@@ -257,3 +257,55 @@ def test_refusals_of_tensors():
                                ([x], g, torch.zeros(3, dtype=torch.int32)), ([x], g, torch.zeros(2)), ([x], torch.zeros(2, 2, 6).transpose(1, 2), None)):
         with pytest.raises((ValueError, TypeError)):
             pkg.dp_relative_bias_grads(ctx, dS, s, True, grads, lengths=lengths)
+
+
+def _additions(L, Tq, Tk, parts):
+    """Additions on the longest path of a score's gradient into its bucket: one per row and layer in a thread; a diagonal's four sums (of two bands,
+    before and after their step over) of at most 256 groups of threads, which share rows of blocks and layers; sixteen lanes to a bucket's diagonals
+    (those of a far band: 15, one per 256 blocks of a row, 6 over the lanes and 8 waves); the parts of a plane, sixteen lanes as well."""
+    return L * Tq + 4 * min(256, L * (Tq // 8 + 1)) + max((Tq + Tk) / 16 + 4, 15 + Tk / 2048 + 14) + 8 + parts / 16 + 5
+
+
+def _check_sums(got, dS, s, both, lengths, causal):
+    ref, most = _grads_reference(dS, s, both, lengths, causal)
+    Tq, Tk = dS[0].shape[2:]
+    err = (got.double().cpu() - ref).abs()
+    assert torch.all(err <= _additions(len(dS), Tq, Tk, Tq / 8 + 1) * U * most), (err / (U * most + 1e-300)).max()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("both,causal", [(True, False), (False, True), (False, False)])
+@pytest.mark.parametrize("Tq,Tk,last", [(3, 32765, 30000), (3, 32765, 1 << 30), (600, 9000, 8700), (2, 8750, 8749), (2, 8700, 8699)])
+def test_grads_whose_diagonals_fill_the_local_memory(dp, Tq, Tk, last, both, causal, dtype):
+    """Last starts so far away that most of the Tq + Tk - 1 diagonals are taken apart: up to 158 KiB of a CU's memory, below and above 64."""
+    starts = [0, 1, 2, 3, 50, 51, 700, last // 2, last - 1, last]
+    dS = _scores(1, 2, 1, Tq, Tk, dtype, Tq + Tk)
+    grads = torch.empty(2, len(starts) * (2 if both else 1), 1, device=DEV)
+    dp.relative_bias_grads(dS, starts, both, grads, causal=causal)
+    dp.sync()
+    _check_sums(grads, dS, starts, both, None, causal)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("padded", [False, True])
+@pytest.mark.parametrize("starts,both", [("t16", False), ("far", True)])
+@pytest.mark.parametrize("T", [2040, 2041, 2049, 2100])
+def test_grads_of_long_squares_under_a_causal_mask(dp, T, starts, both, padded, dtype):
+    """Rows of blocks, two of which are a step, around what the threads of a workgroup hold at a time (256 blocks), with NaN and infinities behind
+    the lengths and the mask."""
+    s = dict(STARTS, far=[0, 1, 5, 16, 900, 2030])[starts]
+    lengths = torch.tensor([T, T - 9, 1030], dtype=torch.int32) if padded else None
+    B = 3 if padded else 1
+    dS = _scores(2, B, 1, T, T, dtype, T)
+    out = (_rel(T, T) > 0).expand(B, 1, T, T)
+    if padded:
+        pos = torch.arange(T)
+        out = out | ~((pos[None, :, None] < lengths[:, None, None]) & (pos[None, None, :] < lengths[:, None, None]))[:, None]
+    dS[0][out.to(DEV)] = float("nan")
+    dS[1][out.to(DEV)] = float("inf")
+    grads = torch.empty(B, len(s) * (2 if both else 1), 1, device=DEV)
+    dp.relative_bias_grads(dS, s, both, grads, lengths=None if lengths is None else lengths.to(DEV), causal=True)
+    dp.sync()
+    _check_sums(grads, dS, s, both, lengths, True)
