@@ -93,6 +93,7 @@ dp_status dp_create(dp_ctx** out, void* hip_stream, size_t workspace_bytes) {
     if (e == hipSuccess) e = hipMemset(ctx->err_word, 0, WORDS);
     if (e == hipSuccess) ctx->ticket = (uint32_t*)ctx->err_word + 32;
     if (e != hipSuccess) {
+        dp_forget_error();
         if (ctx->ws) (void)hipFree(ctx->ws);
         if (ctx->err_word) (void)hipFree(ctx->err_word);
         if (ctx->cbuf) (void)hipFree(ctx->cbuf);

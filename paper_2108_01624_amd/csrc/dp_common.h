@@ -31,6 +31,9 @@ struct dp_ctx {
     char msg[256];
 };
 
+// The runtime keeps a failed call's error until it is asked for: whoever has seen it takes it away, or the next launch's check would report it.
+static inline void dp_forget_error() { (void)hipGetLastError(); }
+
 // Brackets one kernel launch with events when profiling is on (no-op otherwise).
 struct dp_prof_scope {
     dp_ctx* ctx;
@@ -39,18 +42,18 @@ struct dp_prof_scope {
         if (!c->prof_on || c->prof_n >= DP_PROF_CAP) return;
         dp_prof_rec* r = &c->prof[c->prof_n];
         if (c->prof_n >= c->prof_made) {
-            if (hipEventCreate(&r->start) != hipSuccess) return;
-            if (hipEventCreate(&r->stop) != hipSuccess) { (void)hipEventDestroy(r->start); return; }
+            if (hipEventCreate(&r->start) != hipSuccess) { dp_forget_error(); return; }
+            if (hipEventCreate(&r->stop) != hipSuccess) { dp_forget_error(); (void)hipEventDestroy(r->start); return; }
             c->prof_made = c->prof_n + 1;
         }
         r->kind = kind;
         r->work = work;
-        if (hipEventRecord(r->start, c->stream) != hipSuccess) return;
+        if (hipEventRecord(r->start, c->stream) != hipSuccess) { dp_forget_error(); return; }
         rec = r;
         c->prof_n++;
     }
     ~dp_prof_scope() {
-        if (rec) (void)hipEventRecord(rec->stop, ctx->stream);
+        if (rec && hipEventRecord(rec->stop, ctx->stream) != hipSuccess) dp_forget_error();
     }
 };
 
@@ -60,6 +63,7 @@ struct dp_prof_scope {
     do {                                                                             \
         hipError_t e__ = (expr);                                                     \
         if (e__ != hipSuccess) {                                                     \
+            dp_forget_error();                                                       \
             DP_SET_ERR(ctx, "%s failed: %s", #expr, hipGetErrorString(e__));         \
             return DP_ERR_HIP;                                                       \
         }                                                                            \

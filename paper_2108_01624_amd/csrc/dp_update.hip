@@ -381,11 +381,17 @@ dp_status dpk_static_scratch(float** out) {
     static std::mutex mu;
     static float* ptr[MAX_DEV] = {};
     int dev = -1;
-    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= MAX_DEV) return DP_ERR_HIP;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= MAX_DEV) {
+        dp_forget_error();
+        return DP_ERR_HIP;
+    }
     std::lock_guard<std::mutex> lock(mu);
     if (!ptr[dev]) {
         void* p = nullptr;
-        if (hipGetSymbolAddress(&p, HIP_SYMBOL(dp_static_scratch)) != hipSuccess || !p) return DP_ERR_HIP;
+        if (hipGetSymbolAddress(&p, HIP_SYMBOL(dp_static_scratch)) != hipSuccess || !p) {
+            dp_forget_error();
+            return DP_ERR_HIP;
+        }
         ptr[dev] = static_cast<float*>(p);
     }
     *out = ptr[dev];

@@ -1244,6 +1244,7 @@ dp_status dpk_mfma_ceiling(dp_ctx* ctx, int iters, int launches, double* tflops)
     hipEvent_t e0, e1;
     DP_HIP_CHECK(ctx, hipEventCreate(&e0));
     if (hipEventCreate(&e1) != hipSuccess) {
+        dp_forget_error();
         (void)hipEventDestroy(e0);
         DP_SET_ERR(ctx, "hipEventCreate failed");
         return DP_ERR_HIP;
@@ -1259,6 +1260,7 @@ dp_status dpk_mfma_ceiling(dp_ctx* ctx, int iters, int launches, double* tflops)
     (void)hipEventDestroy(e0);
     (void)hipEventDestroy(e1);
     if (e != hipSuccess) {
+        dp_forget_error();
         DP_SET_ERR(ctx, "mfma calibration failed: %s", hipGetErrorString(e));
         return DP_ERR_HIP;
     }
