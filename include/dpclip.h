@@ -244,16 +244,17 @@ dp_status dp_clip_factors(dp_ctx* ctx, const float* sqnorms, int B, float C, flo
  * Tensors of different types go into calls of their own.  Up to 160 tensors share a launch.  With B > 1 counts end at 2^31 (DP_ERR_SHAPE above).
  * ------------------------------------------------------------------------------------------------- */
 
-/* sqnorms[i] += sum_l sum_k X[l][i, k]^2.  The norms of a tensor's pieces pass through the workspace (a float per unit for every tensor,
+/* sqnorms[i] += sum_l sum_k X[l][i, k]^2; sqnorms overlaps no X (DP_ERR_VALUE).  The norms of a tensor's pieces pass through the workspace (a float per unit for every tensor,
  * more for long ones); fewer tensors share a launch where they do not fit, DP_ERR_WORKSPACE if those of one tensor do not. */
 dp_status dp_sqnorms_grads(dp_ctx* ctx, int n_layers, const void* const* X, const uint64_t* counts, dp_dtype dtype, int B, float* sqnorms);
 
-/* sums[l][k] += sum_i c_i X[l][i, k] (fp32).  Tensors whose sums overlap add to them launch after launch; no sum overlaps an X. */
+/* sums[l][k] += sum_i c_i X[l][i, k] (fp32).  Tensors whose sums overlap add to them launch after launch; no sum overlaps an X or sqnorms
+ * (DP_ERR_VALUE). */
 dp_status dp_clip_accumulate_grads(dp_ctx* ctx, int n_layers, const void* const* X, const uint64_t* counts, dp_dtype dtype, int B, float C,
                                    const float* sqnorms, float* const* sums);
 
 /* Y[l][i, k] = c_i X[l][i, k], of X's dtype, rounded once: every unit's gradient clipped to norm C.  Y[l] is X[l] (clipped in place;
- * units whose norm is within C are then not touched) or overlaps no X and no other Y. */
+ * units whose norm is within C are then not touched) or overlaps no X; it overlaps no other Y and not sqnorms (DP_ERR_VALUE). */
 dp_status dp_clip_grads(dp_ctx* ctx, int n_layers, const void* const* X, const uint64_t* counts, dp_dtype dtype, int B, float C,
                         const float* sqnorms, void* const* Y);
 

@@ -5,6 +5,8 @@
 #include <stdlib.h>
 #include <string.h>
 
+#include <algorithm>
+
 #include "dp_common.h"
 
 namespace {
@@ -66,6 +68,54 @@ dp_status check_sum_width(dp_ctx* ctx, dp_dtype dt, int d_in, int d_out) {
         dp_status s__ = (expr);      \
         if (s__ != DP_OK) return s__; \
     } while (0)
+
+// A range of memory, from its first byte to the one behind its last.
+struct Span {
+    uintptr_t from, to;
+    bool output;
+    bool meets(const Span& o) const { return from < o.to && o.from < to; }
+};
+
+// Whether one of n ranges that are written meets one that is read or (`apart`) another that is written.  in(l), out(l): range l (from == to: none).
+// A flat buffer of outputs is seen through by one look at every range; ranges of outputs and inputs in any order are sorted.
+template <typename In, typename Out>
+dp_status spans_apart(dp_ctx* ctx, int n, const Span& also_read, In in, Out out, bool apart) {
+    Span hull = {UINTPTR_MAX, 0, true};
+    bool rising = true;
+    for (int l = 0; l < n; ++l) {
+        const Span o = out(l);
+        if (o.from == o.to) continue;
+        rising = rising && o.from >= hull.to;
+        hull.from = o.from < hull.from ? o.from : hull.from;
+        hull.to = o.to > hull.to ? o.to : hull.to;
+    }
+    if (hull.to == 0) return DP_OK;
+    int within = also_read.meets(hull) ? 1 : 0;
+    for (int l = 0; l < n; ++l) within += in(l).meets(hull) ? 1 : 0;
+    if (within == 0 && (rising || !apart)) return DP_OK;
+    Span* const s = (Span*)malloc((2 * (size_t)n + 1) * sizeof(Span));
+    if (!s) FAIL(ctx, DP_ERR_HIP, "no host memory to compare the ranges of %d tensors", n);
+    size_t m = 0;
+    auto put = [&](const Span& x) {
+        if (x.from != x.to) s[m++] = x;
+    };
+    put(also_read);
+    for (int l = 0; l < n; ++l) {
+        put(in(l));
+        put(out(l));
+    }
+    std::sort(s, s + m, [](const Span& a, const Span& b) { return a.from < b.from; });
+    uintptr_t read = 0, written = 0;  // ends of the ranges that begin before the next one
+    bool meet = false;
+    for (size_t k = 0; k < m && !meet; ++k) {
+        meet = s[k].output ? read > s[k].from || (apart && written > s[k].from) : written > s[k].from;
+        uintptr_t& end = s[k].output ? written : read;
+        end = s[k].to > end ? s[k].to : end;
+    }
+    free(s);
+    if (meet) FAIL(ctx, DP_ERR_VALUE, apart ? "an output overlaps an input, or another output" : "a sum overlaps an input");
+    return DP_OK;
+}
 
 }  // namespace
 
@@ -446,29 +496,43 @@ dp_status dp_clip_factors(dp_ctx* ctx, const float* sqnorms, int B, float C, flo
     return dpk_clip_factors(ctx, sqnorms, B, C, c);
 }
 
-// Tensors of held gradients; `out` may be NULL (a call without outputs).
+// Tensors of held gradients; `out` may be NULL (a call without outputs).  SUMS: outputs are a unit's fp32 sums, which may share memory; otherwise of
+// the inputs' size and type, each apart from all others or in place of its input.
+enum HeldOut { HELD_NONE, HELD_SUMS, HELD_SCALED };
 static dp_status check_grads(dp_ctx* ctx, int n, const void* const* X, const uint64_t* counts, dp_dtype dtype, int B, const float* sqnorms, const void* const* out,
-                             int out_align) {
+                             HeldOut kind) {
     TRY(check_dtype(ctx, dtype));
     if (n < 0 || B < 0) FAIL(ctx, DP_ERR_SHAPE, "negative count");
     if (n > 0 && (!X || !counts)) FAIL(ctx, DP_ERR_NULL, "a table is NULL");
     if (B == 0) return DP_OK;  // (tensors of no elements have no address)
-    const uintptr_t low = dtype == DP_BF16 ? 1 : 3;
+    const size_t elem = dtype == DP_BF16 ? 2 : 4, out_elem = kind == HELD_SUMS ? 4 : elem;
     for (int l = 0; l < n; ++l) {
         if (counts[l] == 0) continue;
         if (counts[l] > (B > 1 ? 1ull << 31 : 1ull << 59)) FAIL(ctx, DP_ERR_SHAPE, "counts[%d] is too large", l);
         if (!X[l]) FAIL(ctx, DP_ERR_NULL, "X[%d] is NULL", l);
-        if ((uintptr_t)X[l] & low) FAIL(ctx, DP_ERR_ALIGN, "X[%d] is not aligned to its elements", l);
-        if (!out) continue;
+        if ((uintptr_t)X[l] & (elem - 1)) FAIL(ctx, DP_ERR_ALIGN, "X[%d] is not aligned to its elements", l);
+        if (kind == HELD_NONE) continue;
         if (!out[l]) FAIL(ctx, DP_ERR_NULL, "output %d is NULL", l);
-        if ((uintptr_t)out[l] & (uintptr_t)(out_align - 1)) FAIL(ctx, DP_ERR_ALIGN, "output %d is not aligned to its elements", l);
+        if ((uintptr_t)out[l] & (out_elem - 1)) FAIL(ctx, DP_ERR_ALIGN, "output %d is not aligned to its elements", l);
     }
-    return check_f32(ctx, "sqnorms", sqnorms);
+    TRY(check_f32(ctx, "sqnorms", sqnorms));
+    const Span norms = {(uintptr_t)sqnorms, (uintptr_t)(sqnorms + B), kind == HELD_NONE};
+    auto in = [&](int l) -> Span { return {(uintptr_t)X[l], counts[l] ? (uintptr_t)X[l] + counts[l] * B * elem : (uintptr_t)X[l], false}; };
+    if (kind == HELD_NONE) {
+        for (int l = 0; l < n; ++l)
+            if (counts[l] && in(l).meets(norms)) FAIL(ctx, DP_ERR_VALUE, "sqnorms overlaps X[%d]", l);
+        return DP_OK;
+    }
+    if (kind == HELD_SUMS)
+        return spans_apart(ctx, n, norms, in, [&](int l) -> Span { return {(uintptr_t)out[l], (uintptr_t)out[l] + counts[l] * 4, true}; }, false);
+    // (in place: the output alone stands for both)
+    return spans_apart(ctx, n, norms, [&](int l) -> Span { return X[l] == out[l] ? Span{0, 0, false} : in(l); },
+                       [&](int l) -> Span { return {(uintptr_t)out[l], (uintptr_t)out[l] + counts[l] * B * elem, true}; }, true);
 }
 
 dp_status dp_sqnorms_grads(dp_ctx* ctx, int n_layers, const void* const* X, const uint64_t* counts, dp_dtype dtype, int B, float* sqnorms) {
     REQUIRE_CTX(ctx);
-    TRY(check_grads(ctx, n_layers, X, counts, dtype, B, sqnorms, nullptr, 1));
+    TRY(check_grads(ctx, n_layers, X, counts, dtype, B, sqnorms, nullptr, HELD_NONE));
     if (B == 0 || n_layers == 0) return DP_OK;
     return dpk_held_sqnorms(ctx, n_layers, X, counts, dtype, B, sqnorms);
 }
@@ -477,7 +541,7 @@ dp_status dp_clip_accumulate_grads(dp_ctx* ctx, int n_layers, const void* const*
                                    const float* sqnorms, float* const* sums) {
     REQUIRE_CTX(ctx);
     if (n_layers > 0 && !sums) FAIL(ctx, DP_ERR_NULL, "a table is NULL");
-    TRY(check_grads(ctx, n_layers, X, counts, dtype, B, sqnorms, (const void* const*)sums, 4));
+    TRY(check_grads(ctx, n_layers, X, counts, dtype, B, sqnorms, (const void* const*)sums, HELD_SUMS));
     TRY(check_clip(ctx, C, 0));
     if (B == 0 || n_layers == 0) return DP_OK;
     return dpk_held_sums(ctx, n_layers, X, counts, dtype, B, C, sqnorms, sums);
@@ -487,7 +551,7 @@ dp_status dp_clip_grads(dp_ctx* ctx, int n_layers, const void* const* X, const u
                         const float* sqnorms, void* const* Y) {
     REQUIRE_CTX(ctx);
     if (n_layers > 0 && !Y) FAIL(ctx, DP_ERR_NULL, "a table is NULL");
-    TRY(check_grads(ctx, n_layers, X, counts, dtype, B, sqnorms, Y, dtype == DP_BF16 ? 2 : 4));
+    TRY(check_grads(ctx, n_layers, X, counts, dtype, B, sqnorms, Y, HELD_SCALED));
     TRY(check_clip(ctx, C, 0));
     if (B == 0 || n_layers == 0) return DP_OK;
     return dpk_held_scale(ctx, n_layers, X, counts, dtype, B, C, sqnorms, Y);

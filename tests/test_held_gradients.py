@@ -214,3 +214,81 @@ def test_refusals_of_tensors():
         pkg.dp_sqnorms_grads(ctx, [x.half()], sq)
     with pytest.raises(TypeError):
         pkg.dp_sqnorms_grads(ctx, [x], sq.double())
+
+
+def test_refusals_of_outputs_that_overlap():
+    """Outputs over inputs, norms or each other: refused before anything is launched, wherever in the call the two tensors stand.  What is allowed goes
+    on to its launch, which fails for want of a GPU (-8)."""
+    import paper_2108_01624_amd as pkg
+
+    if torch.cuda.is_available():
+        pytest.skip("on the CPU, where no call could touch memory")
+    lib = pkg.load_library()
+    ctx = ctypes.create_string_buffer(1 << 14)
+    keep = np.zeros(1 << 16, dtype=np.float32)
+    p = keep.ctypes.data
+    sq = p + 4 * 60000
+    tab = lambda a: (ctypes.c_void_p * len(a))(*a)
+    cnt = lambda a: (ctypes.c_uint64 * len(a))(*a)
+    F, H = pkg.DP_F32, pkg.DP_BF16
+
+    def scale(X, Y, counts, B=2, dt=F, sq=sq):
+        return lib.dp_clip_grads(ctx, len(X), tab(X), cnt(counts), dt, B, 1.0, sq, tab(Y))
+
+    def sums(X, S, counts, B=2, dt=F, sq=sq):
+        return lib.dp_clip_accumulate_grads(ctx, len(X), tab(X), cnt(counts), dt, B, 1.0, sq, tab(S))
+
+    at = lambda *floats: [p + 4 * f for f in floats]
+    for order in (1, -1):
+        o = lambda a: a[::order]
+        # 40 tensors of 2 x 10 numbers: X at 0, 20, ..., Y behind them
+        X, Y = at(*range(0, 800, 20)), at(*range(800, 1600, 20))
+        assert scale(o(X), o(Y), [10] * 40) == -8 and scale(o(X), o(X), [10] * 40) == -8 and scale(X, X[:20] + Y[20:], [10] * 40) == -8
+        assert scale(o(Y), o(X), [10] * 40) == -8 and sums(o(X), o(Y), [10] * 40) == -8 and sums(X, Y[::-1], [10] * 40) == -8
+        assert scale(o(X[:-1] + X[:1]), o(X[:-1] + X[:1]), [10] * 40) == -5        # a tensor listed twice, in place
+        assert scale(X, o(Y[:-1] + Y[:1]), [10] * 40) == -5                        # one output for two
+        assert scale(X, o(Y[:7] + [Y[7] + 4] + Y[8:]), [10] * 40) == -5            # an output that reaches into the next
+        assert scale(X, o(Y[:7] + [X[39]] + Y[8:]), [10] * 40) == -5               # ... or over another tensor's input
+        assert scale(o(X), o([X[0] + 4] + Y[1:]), [10] * 40) == -5                 # in place, but for one number
+        assert scale(X, X[1:] + [X[0]], [10] * 40) == -5
+        assert sums(X, o(Y[:39] + [X[3] + 76]), [10] * 40) == -5                   # the last number of an input
+        assert sums(X, o(Y[:39] + [X[3] - 36]), [10] * 40) == -5                   # the first
+        assert sums(X[1:], o(Y[:38] + [X[0]]), [10] * 39) == -8                    # in front of all of them
+        assert sums(X, o(Y[:39] + Y[:1]), [10] * 40) == -8                         # sums may share
+        assert scale(X, Y, [10] * 39 + [0]) == -8 and scale(X, o(Y[:39] + X[3:4]), o([10] * 39 + [0])) == -8   # (a tensor of no elements has no place)
+        assert scale(X, o(Y), [10] * 40, sq=Y[5] + 76) == -5 and sums(X, o(Y), [10] * 40, sq=Y[5] + 36) == -5 and scale(o(X), o(X), [10] * 40, sq=X[5]) == -5
+        assert scale(X, o(Y), [10] * 40, sq=Y[39] + 80) == -8 and sums(X, o(Y), [10] * 40, sq=X[7]) == -8
+    # bf16 ranges are half as long, sums are not
+    assert scale(at(0, 10), at(20, 30), [10, 10], dt=H) == -8 and scale(at(0, 10), at(19, 30), [10, 10], dt=H) == -5
+    assert sums(at(0, 10), at(20, 30), [10, 10], dt=H) == -8 and sums(at(0, 10), at(19, 30), [10, 10], dt=H) == -5 and sums(at(20), at(11), [10], dt=H) == -5
+    assert sums(at(20), at(10), [10], dt=H) == -8
+    norms = lambda sq, dt=F, B=2, counts=(10, 10): lib.dp_sqnorms_grads(ctx, 2, tab(at(0, 100)), cnt(counts), dt, B, sq)
+    assert norms(p + 76) == -5 and norms(p + 4 * 99) == -5 and norms(p + 4 * 119) == -5 and norms(p + 40, dt=H, counts=(10, 0)) != -5
+    assert norms(p + 80) != -5 and norms(p + 4 * 98) != -5 and norms(p + 4 * 120) != -5 and norms(p + 4 * 100, counts=(10, 0)) != -5
+
+
+@pytest.mark.gpu
+def test_a_tied_tensor_in_place_is_refused_and_left_alone(dp):
+    import paper_2108_01624_amd as pkg
+
+    Xs = _tensors(3, (5000, 700), "bf16", 11)
+    before = [t.clone() for t in Xs]
+    sq = torch.full((3,), 100.0, device=DEV)
+    for outs in ([Xs[0], Xs[1], Xs[0]], [torch.empty_like(Xs[0]), Xs[0].flatten()[:2100].view(3, 700), Xs[0]]):
+        with pytest.raises(pkg.DpError) as e:
+            dp.clip_grads([Xs[0], Xs[1], Xs[0]], 1.0, sq, outs)
+        assert e.value.status == -5
+    buf = torch.zeros(5000 + 700, device=DEV)
+    with pytest.raises(pkg.DpError) as e:
+        dp.clip_accumulate_grads([buf[:5000].view(1, 5000), torch.zeros(1, 700, device=DEV)], 1.0, sq[:1], [torch.zeros(5000, device=DEV), buf[4999:-1]])
+    assert e.value.status == -5
+    dp.sync()
+    assert all(torch.equal(a, b) for a, b in zip(Xs, before)) and not buf.any()
+    # what does not meet is taken: every second tensor of a buffer in place, the others beside their inputs
+    flat = torch.randn(8, 3, 1000, device=DEV)
+    X = list(flat)
+    Y = [x if k % 2 else torch.empty_like(x) for k, x in enumerate(X)]
+    want = [x * 0.1 for x in X]
+    dp.clip_grads(X, 1.0, sq, Y)
+    dp.sync()
+    assert all(((y - w).abs() <= 40 * U * w.abs()).all() for y, w in zip(Y, want))
