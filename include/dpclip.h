@@ -244,8 +244,9 @@ dp_status dp_clip_factors(dp_ctx* ctx, const float* sqnorms, int B, float C, flo
  * Tensors of different types go into calls of their own.  Up to 160 tensors share a launch.  With B > 1 counts end at 2^31 (DP_ERR_SHAPE above).
  * ------------------------------------------------------------------------------------------------- */
 
-/* sqnorms[i] += sum_l sum_k X[l][i, k]^2; sqnorms overlaps no X (DP_ERR_VALUE).  The norms of a tensor's pieces pass through the workspace (a float per unit for every tensor,
- * more for long ones); fewer tensors share a launch where they do not fit, DP_ERR_WORKSPACE if those of one tensor do not. */
+/* sqnorms[i] += sum_l sum_k X[l][i, k]^2; sqnorms overlaps no X (DP_ERR_VALUE).  The norms of a tensor's pieces pass
+ * through the workspace (a float per unit for every tensor, more for long ones); fewer tensors share a launch where they do not fit,
+ * DP_ERR_WORKSPACE if those of one tensor do not. */
 dp_status dp_sqnorms_grads(dp_ctx* ctx, int n_layers, const void* const* X, const uint64_t* counts, dp_dtype dtype, int B, float* sqnorms);
 
 /* sums[l][k] += sum_i c_i X[l][i, k] (fp32).  Tensors whose sums overlap add to them launch after launch; no sum overlaps an X or sqnorms
@@ -296,7 +297,8 @@ dp_status dp_relative_bias_grads(dp_ctx* ctx, int n_layers, const void* const* d
  *   q, k: [B, T, Hq, D] and [B, T, Hk, D] of `dtype`, a token's heads next to each other, tokens ldq / ldk numbers apart (at least Hq D / Hk D;
  *   more where they are parts of a fused projection's output).  Either may have no heads (its pointers are not looked at).  Element alignment.
  *   D in [8, 512] and R in [0, D], both multiples of 8; eps a positive normal number; n_pos >= 1 if R > 0.  The range of memory that an
- *   output lies in meets no input's (DP_ERR_VALUE).  Arithmetic in fp32.
+ *   output lies in meets no input's and no other output's (DP_ERR_VALUE), but that dq and dk may be different columns of the same rows
+ *   (ldq == ldk).  Arithmetic in fp32.
  * ------------------------------------------------------------------------------------------------- */
 
 /* yq [B, T, Hq, D], yk [B, T, Hk, D], dense. */

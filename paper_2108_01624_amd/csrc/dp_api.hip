@@ -644,12 +644,6 @@ dp_status dp_relative_bias_grads(dp_ctx* ctx, int n_layers, const void* const* d
     return dpk_relbias_grads(ctx, n_layers, dS, dtype, lengths, causal != 0, n, starts, bidirectional != 0, B, H, Tq, Tk, grads);
 }
 
-// Whether the places of `tokens` tokens, `ld` numbers apart and `width` long, lie in one range of memory with another such tensor's.
-static bool spans_meet(const void* a, long tokens, int64_t lda, long wa, const void* b, int64_t ldb, long wb, size_t elem) {
-    const uintptr_t a0 = (uintptr_t)a, b0 = (uintptr_t)b, a1 = a0 + ((size_t)(tokens - 1) * lda + wa) * elem, b1 = b0 + ((size_t)(tokens - 1) * ldb + wb) * elem;
-    return a && b && a0 < b1 && b0 < a1;
-}
-
 static dp_status check_qk(dp_ctx* ctx, const dp_qk_args& a) {
     TRY(check_dtype(ctx, a.dtype));
     TRY(check_bt(ctx, a.B, a.T));
@@ -677,16 +671,53 @@ static dp_status check_qk(dp_ctx* ctx, const dp_qk_args& a) {
     return DP_OK;
 }
 
-// An output of H heads per token: where it is wanted, aligned and apart from the inputs.
-static dp_status check_qk_out(dp_ctx* ctx, const dp_qk_args& a, const char* name, const void* y, int H, int64_t ld, const void* dyq, const void* dyk) {
-    if (H == 0 || a.B == 0 || a.T == 0) return DP_OK;
+// The range of memory that `tokens` tokens of `width` numbers lie in, `ld` numbers apart.
+static Span tokens_span(const void* p, long tokens, int64_t ld, long width, size_t elem, bool output) {
+    return {(uintptr_t)p, (uintptr_t)p + ((size_t)(tokens - 1) * ld + width) * elem, output};
+}
+
+// Outputs of heads (of the queries, of the keys; ldq, ldk numbers from token to token) and `grads`, if there are any: aligned, and apart from each other
+// and from what is read.
+static dp_status check_qk_out(dp_ctx* ctx, const dp_qk_args& a, const char* const names[2], const void* const y[2], const int64_t ld[2], const void* dyq, const void* dyk,
+                              const float* grads) {
     const size_t e = a.dtype == DP_BF16 ? 2 : 4;
-    const long n = (long)a.B * a.T, D = a.D;
-    if (!y) FAIL(ctx, DP_ERR_NULL, "%s is NULL", name);
-    if ((uintptr_t)y & (e - 1)) FAIL(ctx, DP_ERR_ALIGN, "%s is not aligned to its elements", name);
-    if ((a.Hq && spans_meet(y, n, ld, H * D, a.q, a.ldq, a.Hq * D, e)) || (a.Hk && spans_meet(y, n, ld, H * D, a.k, a.ldk, a.Hk * D, e)) ||
-        (a.Hq && spans_meet(y, n, ld, H * D, dyq, a.Hq * D, a.Hq * D, e)) || (a.Hk && spans_meet(y, n, ld, H * D, dyk, a.Hk * D, a.Hk * D, e)))
-        FAIL(ctx, DP_ERR_VALUE, "%s overlaps an input", name);
+    const long n = (long)a.B * a.T, w[2] = {(long)a.Hq * a.D, (long)a.Hk * a.D};
+    auto block = [](const void* p, size_t bytes) -> Span { return {(uintptr_t)p, (uintptr_t)p + bytes, false}; };
+    Span read[9], out[3];
+    int n_read = 0, n_out = 0;
+    if (w[0]) read[n_read++] = tokens_span(a.q, n, a.ldq, w[0], e, false);
+    if (w[1]) read[n_read++] = tokens_span(a.k, n, a.ldk, w[1], e, false);
+    if (w[0] && dyq) read[n_read++] = tokens_span(dyq, n, w[0], w[0], e, false);
+    if (w[1] && dyk) read[n_read++] = tokens_span(dyk, n, w[1], w[1], e, false);
+    if (w[0]) read[n_read++] = block(a.gain_q, a.D * sizeof(float));
+    if (w[1]) read[n_read++] = block(a.gain_k, a.D * sizeof(float));
+    if (a.R) read[n_read++] = block(a.cos, (size_t)a.n_pos * (a.R / 2) * sizeof(float));
+    if (a.R) read[n_read++] = block(a.sin, (size_t)a.n_pos * (a.R / 2) * sizeof(float));
+    if (a.R && a.positions) read[n_read++] = block(a.positions, n * sizeof(int32_t));
+    int heads[2];  // place of y[s] in out
+    for (int s = 0; s < 2; ++s) {
+        heads[s] = -1;
+        if (!y || !w[s]) continue;
+        if (!y[s]) FAIL(ctx, DP_ERR_NULL, "%s is NULL", names[s]);
+        if ((uintptr_t)y[s] & (e - 1)) FAIL(ctx, DP_ERR_ALIGN, "%s is not aligned to its elements", names[s]);
+        heads[s] = n_out;
+        out[n_out++] = tokens_span(y[s], n, ld[s], w[s], e, true);
+    }
+    if (grads) out[n_out++] = block(grads, (size_t)a.B * 2 * a.D * sizeof(float));
+    for (int i = 0; i < n_out; ++i) {
+        const char* name = i == heads[0] ? names[0] : i == heads[1] ? names[1] : "grads";
+        for (int j = 0; j < n_read; ++j)
+            if (out[i].meets(read[j])) FAIL(ctx, DP_ERR_VALUE, "%s overlaps an input", name);
+        for (int j = 0; j < i; ++j) {
+            if (!out[i].meets(out[j])) continue;
+            if (i == heads[1] && j == heads[0] && ld[0] == ld[1]) {  // other columns of the same rows
+                const int low = (uintptr_t)y[0] <= (uintptr_t)y[1] ? 0 : 1;
+                const int64_t column = (int64_t)(((uintptr_t)y[1 - low] - (uintptr_t)y[low]) / e) % ld[0];
+                if (column >= w[low] && column + w[1 - low] <= ld[0]) continue;
+            }
+            FAIL(ctx, DP_ERR_VALUE, "%s overlaps another output", name);
+        }
+    }
     return DP_OK;
 }
 
@@ -696,9 +727,11 @@ dp_status dp_qk_norm(dp_ctx* ctx, const void* q, const void* k, dp_dtype dtype, 
     REQUIRE_CTX(ctx);
     const dp_qk_args a = {q, k, dtype, ldq, ldk, gain_q, gain_k, cos, sin, n_pos, positions, interleaved != 0, B, T, Hq, Hk, D, R, eps};
     TRY(check_qk(ctx, a));
-    TRY(check_qk_out(ctx, a, "yq", yq, Hq, (int64_t)Hq * D, nullptr, nullptr));
-    TRY(check_qk_out(ctx, a, "yk", yk, Hk, (int64_t)Hk * D, nullptr, nullptr));
     if (B == 0 || T == 0 || Hq + Hk == 0) return DP_OK;
+    const char* const names[2] = {"yq", "yk"};
+    const void* const y[2] = {yq, yk};
+    const int64_t ld[2] = {(int64_t)Hq * D, (int64_t)Hk * D};
+    TRY(check_qk_out(ctx, a, names, y, ld, nullptr, nullptr, nullptr));
     return dpk_qk_norm(ctx, a, yq, yk);
 }
 
@@ -716,10 +749,10 @@ dp_status dp_qk_norm_grads(dp_ctx* ctx, const void* q, const void* k, dp_dtype d
     if ((Hq && !dyq) || (Hk && !dyk)) FAIL(ctx, DP_ERR_NULL, "dyq or dyk is NULL");
     if ((Hq && ((uintptr_t)dyq & low)) || (Hk && ((uintptr_t)dyk & low))) FAIL(ctx, DP_ERR_ALIGN, "dyq or dyk is not aligned to its elements");
     const bool wanted = (Hq && dq) || (Hk && dk);
-    if (wanted) {
-        TRY(check_qk_out(ctx, a, "dq", dq, Hq, ldq, dyq, dyk));
-        TRY(check_qk_out(ctx, a, "dk", dk, Hk, ldk, dyq, dyk));
-    }
+    const char* const names[2] = {"dq", "dk"};
+    const void* const y[2] = {dq, dk};
+    const int64_t ld[2] = {ldq, ldk};
+    TRY(check_qk_out(ctx, a, names, wanted ? y : nullptr, ld, dyq, dyk, grads));
     return dpk_qk_norm_grads(ctx, a, dyq, dyk, grads, dq, dk, wanted);
 }
 

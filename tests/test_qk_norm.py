@@ -265,3 +265,48 @@ def test_refusals_of_tensors():
     for grads, dq, dk in ((z(2, 2, 15), None, None), (z(2, 2, 16).double(), None, None), (z(2, 2, 16), z(2, 3, 2, 16), None), (z(2, 2, 16), z(2, 3, 4, 16)[:, :, :2], z(2, 3, 1, 16))):
         with pytest.raises((ValueError, TypeError)):
             pkg.dp_qk_norm_grads(ctx, *good.values(), grads, dq, dk)
+
+
+def test_refusals_of_outputs_that_overlap():
+    """Outputs over what is read, or over each other: refused before anything is launched.  What is allowed goes on to its launch, which fails for want
+    of a GPU (-8)."""
+    import paper_2108_01624_amd as pkg
+
+    if torch.cuda.is_available():
+        pytest.skip("on the CPU, where no call could touch memory")
+    lib = pkg.load_library()
+    ctx = ctypes.create_string_buffer(1 << 14)
+    keep = np.zeros(1 << 14, dtype=np.float32)
+    at = lambda k: keep.ctypes.data + 4 * k
+    # two examples of three tokens, two query heads and one key head of 16 numbers, next to each other in rows of 60; what is read lies below 1,000
+    B, T, Hq, Hk, D, R, ld = 2, 3, 2, 1, 16, 8, 60
+    base = dict(q=at(0), k=at(32), dt=pkg.DP_F32, ldq=ld, ldk=ld, gq=at(400), gk=at(416), cos=at(432), sin=at(448), n_pos=4, pos=at(464), inter=0, B=B, T=T, Hq=Hq, Hk=Hk, D=D,
+                R=R, eps=1e-6)
+    nq, nk = B * T * Hq * D, B * T * Hk * D   # 192, 96
+    forward = lambda yq=at(1000), yk=at(1300), **kw: lib.dp_qk_norm(ctx, *dict(base, **kw).values(), yq, yk)
+    back = lambda g=at(3000), dq=at(2000), dk=at(2032), dyq=at(500), dyk=at(700), **kw: lib.dp_qk_norm_grads(ctx, *dict(base, **kw).values(), dyq, dyk, g, dq, dk)
+    assert forward() == -8 and back() == -8
+    # each other
+    assert forward(yk=at(1000 + nq)) == -8 and forward(yk=at(1000 + nq - 1)) == -5 and forward(yk=at(1000)) == -5
+    assert forward(yk=at(1000 - nk)) == -8 and forward(yk=at(1000 - nk + 1)) == -5
+    # the columns that are free of dq are 32 to 59, of which dk takes 16
+    for k, st in ((31, -5), (32, -8), (44, -8), (45, -5), (59, -5), (60 + 31, -5), (60 + 32, -8), (-16, -8), (-28, -8), (-29, -5), (-15, -5), (5 * 60 + 32, -8)):
+        assert back(dk=at(2000 + k)) == st, k
+    assert back(dk=at(2032), ldk=61) == -5   # other rows
+    assert back(dq=None, dk=None) == -8
+    # gains, angles, positions; the last number of one, the first of the other
+    for name, n in (("gq", 16), ("gk", 16), ("cos", 16), ("sin", 16), ("pos", 6)):
+        for call, out, last in ((forward, "yq", 1000 + nq - 1), (forward, "yk", 1300 + nk - 1), (back, "dq", 2000 + 5 * ld + 31), (back, "dk", 2032 + 5 * ld + 15),
+                                (back, "g", 3000 + B * 2 * D - 1)):
+            first = {"yq": 1000, "yk": 1300, "dq": 2000, "dk": 2032, "g": 3000}[out]
+            assert call(**{name: at(last)}) == -5 and call(**{name: at(first - n + 1)}) == -5, (name, out)
+            if out != "dq":
+                assert call(**{name: at(last + 1)}) == -8, (name, out)
+    # without a rotation nothing is read of the angles and positions
+    assert forward(R=0, cos=at(1000), sin=at(1000), pos=at(1000)) == -8 and back(R=0, cos=at(2000), sin=at(3000), pos=at(3000)) == -8
+    # grads over queries, keys, their gradients and the outputs
+    for g in (0, 31, 5 * ld + 47, 500, 500 + nq - 1, 700, 700 + nk - 1, 2000, 2000 + 5 * ld + 31):
+        assert back(g=at(g)) == -5, g
+    assert back(g=at(500 + nq - 1), dq=None, dk=None) == -5 and back(g=at(2000), dq=None, dk=None) == -8
+    # sides without heads have no places
+    assert forward(Hk=0, k=None, gk=None, yk=None) == -8 and forward(Hk=0, yk=at(1000)) == -8 and back(Hq=0, dq=at(2032), dyq=at(3000), dk=at(2000)) == -8
