@@ -273,7 +273,8 @@ dp_status dp_clip_grads(dp_ctx* ctx, int n_layers, const void* const* X, const u
  * decided in whole numbers.  DP_ERR_VALUE unless 2 <= n <= 128 and n/2 < max_distance <= 2^30. */
 dp_status dp_relative_buckets(int n, int max_distance, int32_t* starts);
 
-/* bias[h, q, k] = table[bucket(k - p), h] for all pairs, [H, Tq, Tk] of `dtype` (rounded once), element alignment; table fp32. */
+/* bias[h, q, k] = table[bucket(k - p), h] for all pairs, [H, Tq, Tk] of `dtype` (rounded once), element alignment; table fp32, which bias
+ * does not overlap (DP_ERR_VALUE). */
 dp_status dp_relative_bias(dp_ctx* ctx, const float* table, int n, const int32_t* starts, int bidirectional, int H, int Tq, int Tk,
                            dp_dtype dtype, void* bias);
 
@@ -283,7 +284,8 @@ dp_status dp_relative_bias(dp_ctx* ctx, const float* table, int n, const int32_t
  * lengths: int32 [B] on the device, or NULL: only queries and keys at positions below lengths[i] count (clamped to [0, Tk]); causal != 0:
  * only keys k <= p.  What lies elsewhere is not used, whatever it holds (NaN of a row that its mask leaves empty).  n_layers == 0 writes
  * zeros.  grads is what dp_sqnorms_grads and dp_clip_accumulate_grads take.  Sums in fp32.  DP_ERR_SHAPE if Tq > Tk or Tq + Tk > 32768.
- * With few examples and heads the parts of a plane pass through the workspace.  dS is a HOST array, read during the call only. */
+ * With few examples and heads the parts of a plane pass through the workspace.  dS is a HOST array, read during the call only; grads overlaps
+ * neither a dS[l] nor lengths (DP_ERR_VALUE). */
 dp_status dp_relative_bias_grads(dp_ctx* ctx, int n_layers, const void* const* dS, dp_dtype dtype, const int32_t* lengths, int causal, int n,
                                  const int32_t* starts, int bidirectional, int B, int H, int Tq, int Tk, float* grads);
 

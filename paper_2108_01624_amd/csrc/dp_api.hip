@@ -76,6 +76,8 @@ struct Span {
     bool meets(const Span& o) const { return from < o.to && o.from < to; }
 };
 
+Span block_span(const void* p, size_t bytes, bool output) { return {(uintptr_t)p, (uintptr_t)p + bytes, output}; }
+
 // Whether one of n ranges that are written meets one that is read or (`apart`) another that is written.  in(l), out(l): range l (from == to: none).
 // A flat buffer of outputs is seen through by one look at every range; ranges of outputs and inputs in any order are sorted.
 template <typename In, typename Out>
@@ -621,7 +623,10 @@ dp_status dp_relative_bias(dp_ctx* ctx, const float* table, int n, const int32_t
     if (H == 0 || Tq == 0) return DP_OK;
     TRY(check_f32(ctx, "table", table));
     if (!bias) FAIL(ctx, DP_ERR_NULL, "bias is NULL");
-    if ((uintptr_t)bias & (dtype == DP_BF16 ? 1 : 3)) FAIL(ctx, DP_ERR_ALIGN, "bias is not aligned to its elements");
+    const size_t e = dtype == DP_BF16 ? 2 : 4;
+    if ((uintptr_t)bias & (e - 1)) FAIL(ctx, DP_ERR_ALIGN, "bias is not aligned to its elements");
+    if (block_span(bias, (size_t)H * Tq * Tk * e, true).meets(block_span(table, (size_t)n * (bidirectional ? 2 : 1) * H * sizeof(float), false)))
+        FAIL(ctx, DP_ERR_VALUE, "bias overlaps the table");
     return dpk_relbias(ctx, table, n, starts, bidirectional != 0, H, Tq, Tk, dtype, bias);
 }
 
@@ -636,11 +641,16 @@ dp_status dp_relative_bias_grads(dp_ctx* ctx, int n_layers, const void* const* d
     const uint64_t out = (uint64_t)B * H * n * (bidirectional ? 2 : 1);
     if (n_layers == 0 || Tq == 0) return dpk_zero_f32(ctx, grads, out);
     if (!dS) FAIL(ctx, DP_ERR_NULL, "a pointer table is NULL");
+    const size_t e = dtype == DP_BF16 ? 2 : 4;
     for (int l = 0; l < n_layers; ++l) {
         if (!dS[l]) FAIL(ctx, DP_ERR_NULL, "dS[%d] is NULL", l);
-        if ((uintptr_t)dS[l] & (dtype == DP_BF16 ? 1 : 3)) FAIL(ctx, DP_ERR_ALIGN, "dS[%d] is not aligned to its elements", l);
+        if ((uintptr_t)dS[l] & (e - 1)) FAIL(ctx, DP_ERR_ALIGN, "dS[%d] is not aligned to its elements", l);
     }
     if (lengths) TRY(check_f32(ctx, "lengths", lengths));
+    const Span written = block_span(grads, out * sizeof(float), true);
+    for (int l = 0; l < n_layers; ++l)
+        if (written.meets(block_span(dS[l], (size_t)B * H * Tq * Tk * e, false))) FAIL(ctx, DP_ERR_VALUE, "grads overlaps dS[%d]", l);
+    if (lengths && written.meets(block_span(lengths, (size_t)B * sizeof(int32_t), false))) FAIL(ctx, DP_ERR_VALUE, "grads overlaps lengths");
     return dpk_relbias_grads(ctx, n_layers, dS, dtype, lengths, causal != 0, n, starts, bidirectional != 0, B, H, Tq, Tk, grads);
 }
 
@@ -682,7 +692,7 @@ static dp_status check_qk_out(dp_ctx* ctx, const dp_qk_args& a, const char* cons
                               const float* grads) {
     const size_t e = a.dtype == DP_BF16 ? 2 : 4;
     const long n = (long)a.B * a.T, w[2] = {(long)a.Hq * a.D, (long)a.Hk * a.D};
-    auto block = [](const void* p, size_t bytes) -> Span { return {(uintptr_t)p, (uintptr_t)p + bytes, false}; };
+    auto block = [](const void* p, size_t bytes) { return block_span(p, bytes, false); };
     Span read[9], out[3];
     int n_read = 0, n_out = 0;
     if (w[0]) read[n_read++] = tokens_span(a.q, n, a.ldq, w[0], e, false);

@@ -309,3 +309,29 @@ def test_grads_of_long_squares_under_a_causal_mask(dp, T, starts, both, padded, 
     dp.relative_bias_grads(dS, s, both, grads, lengths=None if lengths is None else lengths.to(DEV), causal=True)
     dp.sync()
     _check_sums(grads, dS, s, both, lengths, True)
+
+
+def test_refusals_of_outputs_that_overlap():
+    """What is written over what is read: refused before anything is launched.  What is allowed goes on to its launch, which fails for want of a GPU (-8)."""
+    import paper_2108_01624_amd as pkg
+
+    if torch.cuda.is_available():
+        pytest.skip("on the CPU, where no call could touch memory")
+    lib = pkg.load_library()
+    ctx = ctypes.create_string_buffer(1 << 14)
+    keep = np.zeros(2000, dtype=np.float32)
+    at = lambda k: keep.ctypes.data + 4 * k
+    st = (ctypes.c_int32 * 2)(0, 1)
+    F, BF, H, Tq, Tk, B = pkg.DP_F32, pkg.DP_BF16, 3, 4, 5, 2
+    bias = lambda t, out, both=1, dt=F: lib.dp_relative_bias(ctx, t, 2, st, both, H, Tq, Tk, dt, out)
+    # a table of 12 numbers (6 without buckets behind the query), a bias of 60
+    assert bias(at(0), at(12)) == -8 and bias(at(0), at(11)) == -5 and bias(at(0), at(6), both=0) == -8 and bias(at(0), at(5), both=0) == -5
+    assert bias(at(60), at(0)) == -8 and bias(at(59), at(0)) == -5 and bias(at(30), at(0), dt=BF) == -8 and bias(at(29), at(0), dt=BF) == -5
+    # 24 gradients, scores of 120 numbers, two lengths
+    def grads(g, x, ln=None, dt=F):
+        return lib.dp_relative_bias_grads(ctx, len(x), (ctypes.c_void_p * len(x))(*x), dt, ln, 0, 2, st, 1, B, H, Tq, Tk, g)
+
+    x = [at(k) for k in (0, 120, 240)]
+    assert grads(at(360), x) == -8 and grads(at(359), x) == -5 and grads(at(120), x) == -5 and grads(at(120), x[::2]) == -8 and grads(at(97), x[1:]) == -5
+    assert grads(at(96), x[1:]) == -8 and grads(at(60), x[:1], dt=BF) == -8 and grads(at(59), x[:1], dt=BF) == -5
+    assert grads(at(360), x, ln=at(384)) == -8 and grads(at(360), x, ln=at(383)) == -5 and grads(at(360), x, ln=at(359)) == -5 and grads(at(400), x, ln=at(398)) == -8
