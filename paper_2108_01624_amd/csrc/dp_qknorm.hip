@@ -264,7 +264,7 @@ __global__ __launch_bounds__(256) void qk_norm_grads_kernel(QkArgs A) {
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane % LPH;
     const Place<LPH> L(S, lane);
     const int ex = block / (unsigned)S.chunks, ch = block - ex * S.chunks;
-    const int t0 = ch * S.per, n = !S.H ? 0 : t0 + S.per < A.T ? S.per : A.T - t0;  // tokens t0 .. t0 + n - 1
+    const int t0 = ch * S.per, n = !S.H ? 0 : A.T - t0 < S.per ? A.T - t0 : S.per;  // tokens t0 .. t0 + n - 1
     const Part P = part_of<INTER, ALL>(A, c);
     const long x_off = L.token * S.ld + (long)L.head * A.D, y_off = (long)(L.token * S.H + L.head) * A.D;
     const float inv = 1.f / (float)A.D;
@@ -485,11 +485,11 @@ dp_status dpk_qk_norm_grads(dp_ctx* ctx, const dp_qk_args& a, const void* dyq, c
     uint64_t grid = 0;
     for (Side& S : A.s) {
         if (direct) S.chunks = 1;
-        S.per = (a.T + S.chunks - 1) / S.chunks;
-        S.chunks = (a.T + S.per - 1) / S.per;
+        S.per = (int)(((long)a.T + S.chunks - 1) / S.chunks);
+        S.chunks = (int)(((long)a.T + S.per - 1) / S.per);
         S.blocks = (unsigned)S.chunks * (unsigned)a.B;
         grid += (uint64_t)S.chunks * a.B;
-        if ((long)S.per * S.rpt > 0x7FFFFFFFl) {
+        if ((long)S.per * S.rpt > 0x7FFFFFFFl - 8 * U) {  // (a wave counts two steps ahead)
             DP_SET_ERR(ctx, "too many heads of one example");
             return DP_ERR_SHAPE;
         }

@@ -93,3 +93,29 @@ def test_queries_and_keys(dp):
     assert torch.equal(out[0], yq[-1:]) and torch.equal(out[1], yk[-1:]) and torch.equal(d1, dx[-1:])
     size = torch.stack([dyq[-1].float().abs().sum((0, 1)), dyk[-1].float().abs().sum((0, 1))]) * 8   # a normalised number is below 8 here
     assert torch.all((grads[-1] - g1[0]).abs() <= 2 * (T + 100) * 2.0 ** -24 * size)
+
+
+def test_queries_of_an_example_of_two_billion_tokens(dp):
+    """Nearly 2^31 tokens of one example: the first and last ones, which alone have a gradient, against the same calls on a copy of them, and the gain's
+    gradient against its sum in 64 bits (2,000 terms, a rounding each for u, xhat, their product and the sum)."""
+    T, D, n = (1 << 31) - 5000, 8, 1000
+    q = _pattern(T * D, torch.bfloat16, 7).view(1, T, 1, D)
+    none = torch.empty(1, T, 0, D, dtype=torch.bfloat16, device=DEV)
+    g = torch.linspace(0.5, 2, D, device=DEV)
+    y, dy, grads = torch.empty_like(q), torch.zeros_like(q), torch.empty(1, 2, D, device=DEV)
+    dy[:, :n] = q[:, 5 * n:6 * n]
+    dy[:, -n:] = q[:, 7 * n:8 * n]
+    ends = lambda t: torch.cat([t[:, :n], t[:, -n:]], 1)
+    x, d = ends(q), ends(dy)
+    few, y1, dx1, g1 = none[:, :2 * n], torch.empty_like(x), torch.empty_like(x), torch.empty_like(grads)
+    dp.qk_norm(q, none, g, g, None, None, y, none)
+    dp.qk_norm(x, few, g, g, None, None, y1, few)
+    dp.sync()
+    assert torch.equal(ends(y), y1)
+    dp.qk_norm_grads(q, none, g, g, None, None, dy, none, grads, y, none)
+    dp.qk_norm_grads(x, few, g, g, None, None, d, few, g1, dx1, few)
+    dp.sync()
+    assert torch.equal(ends(y), dx1) and not y[:, n:n + 5000].any() and not y[:, -2 * n:-n].any()
+    x, d = x.double().flatten(0, 2), d.double().flatten(0, 2)
+    terms = d * x * (x.pow(2).mean(-1, keepdim=True) + 1e-6).rsqrt()
+    assert torch.all((grads[0, 0].double() - terms.sum(0)).abs() <= (2 * n + 40) * 2.0 ** -24 * terms.abs().sum(0)) and not grads[0, 1].any()

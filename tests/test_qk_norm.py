@@ -310,3 +310,18 @@ def test_refusals_of_outputs_that_overlap():
     assert back(g=at(500 + nq - 1), dq=None, dk=None) == -5 and back(g=at(2000), dq=None, dk=None) == -8
     # sides without heads have no places
     assert forward(Hk=0, k=None, gk=None, yk=None) == -8 and forward(Hk=0, yk=at(1000)) == -8 and back(Hq=0, dq=at(2032), dyq=at(3000), dk=at(2000)) == -8
+
+
+def test_examples_of_more_than_a_billion_tokens_are_not_refused():
+    """Without room in the workspace an example is one workgroup's: its launch is tried, and fails for want of a GPU (-8)."""
+    import paper_2108_01624_amd as pkg
+
+    if torch.cuda.is_available():
+        pytest.skip("on the CPU, where no call could touch memory")
+    lib = pkg.load_library()
+    ctx = ctypes.create_string_buffer(1 << 14)
+    at = lambda k: k << 44
+    for T in (1 << 30, (1 << 30) + 1, (1 << 31) - 5000, (1 << 31) - 4097):
+        args = (at(1), None, pkg.DP_BF16, 8, 8, at(2), None, None, None, 0, None, 0, 1, T, 1, 0, 8, 0, 1e-6)
+        assert lib.dp_qk_norm(ctx, *args, at(3), None) == -8, T
+        assert lib.dp_qk_norm_grads(ctx, *args, at(4), None, at(5), at(6), None) == -8, T
