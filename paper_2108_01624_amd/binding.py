@@ -428,6 +428,12 @@ def _where(*tensors):
             raise ValueError(f"tensors on {dev} and {t.device} in one call")
 
 
+def _ints(where, *sizes):
+    """Refuses sizes that an argument of the library does not hold (ctypes would keep 32 bits of them)."""
+    if max(sizes) > 0x7FFFFFFF:
+        raise DpError(-2, where, f"sizes {sizes}: at most 2^31 - 1 each")
+
+
 def _dense(what, t):
     if not t.is_contiguous():
         raise ValueError(f"{what}: a dense (contiguous) tensor expected")
@@ -444,6 +450,7 @@ def _held(Xs, sqnorms, outs, what, whole):
         raise ValueError(f"{len(outs)} {what} for {len(Xs)} tensors")
     _where(sqnorms, *Xs, *(outs or ()))
     n = len(Xs)
+    _ints("gradients", n, B)
     counts, ptrs, out_ptrs = [], [], []
     dt = Xs[0].dtype if n else sqnorms.dtype
     for k, x in enumerate(Xs):
@@ -484,13 +491,21 @@ def dp_clip_grads(ctx, Xs, C, sqnorms, Ys):
 
 def dp_relative_buckets(n, max_distance) -> list:
     """The first distances of n buckets of a side, half of them one distance each, the others in equal steps of the logarithm (host only)."""
-    if n > 128:
-        raise DpError(-5, "dp_relative_buckets", "at most 128 buckets of a side")
+    # (ctypes cuts numbers down to the 32 bits of an argument; the library judges what fits)
+    if n > 128 or n < 0 or abs(max_distance) > 1 << 30:
+        raise DpError(-5, "dp_relative_buckets", "2 to 128 buckets of a side, and distances up to 2^30")
     buf = (ctypes.c_int32 * max(n, 1))()
     st = load_library().dp_relative_buckets(n, max_distance, buf)
     if st != DP_OK:
         raise DpError(st, "dp_relative_buckets")
     return list(buf)
+
+
+def _starts(starts, where):
+    """HOST array of the buckets' first distances."""
+    if any(abs(s) > 1 << 30 for s in starts):   # (ctypes would keep 32 bits of a number, whatever they are)
+        raise DpError(-5, where, f"starts {list(starts)}: none below the one before it, none above 2^30")
+    return (ctypes.c_int32 * len(starts))(*starts)
 
 
 def dp_relative_bias(ctx, table, starts, bidirectional, bias):
@@ -499,7 +514,8 @@ def dp_relative_bias(ctx, table, starts, bidirectional, bias):
     if tuple(table.shape) != (n * (2 if bidirectional else 1), H):
         raise ValueError(f"table of shape {tuple(table.shape)}: [{n * (2 if bidirectional else 1)}, {H}] expected")
     _where(table, bias)
-    st = load_library().dp_relative_bias(ctx, _f32(_dense("table", table)), n, (ctypes.c_int32 * n)(*starts), int(bool(bidirectional)), H, Tq, Tk,
+    _ints("dp_relative_bias", H, Tq, Tk)
+    st = load_library().dp_relative_bias(ctx, _f32(_dense("table", table)), n, _starts(starts, "dp_relative_bias"), int(bool(bidirectional)), H, Tq, Tk,
                                          _dtype_of(bias), _dense("bias", bias).data_ptr())
     _check(ctx, st, "dp_relative_bias")
 
@@ -517,9 +533,10 @@ def dp_relative_bias_grads(ctx, dSs, starts, bidirectional, grads, *, lengths=No
     if lengths is not None and tuple(lengths.shape) != (B,):
         raise ValueError(f"lengths of shape {tuple(lengths.shape)}: ({B},) expected")
     _where(grads, lengths, *dSs)
+    _ints("dp_relative_bias_grads", len(dSs), B, H, Tq, Tk)
     st = load_library().dp_relative_bias_grads(
         ctx, len(dSs), _table([x.data_ptr() for x in dSs], len(dSs)), _dtype_code(dt), _i32(None if lengths is None else _dense("lengths", lengths)),
-        int(bool(causal)), n, (ctypes.c_int32 * n)(*starts), int(bool(bidirectional)), B, H, Tq, Tk, _f32(_dense("grads", grads)))
+        int(bool(causal)), n, _starts(starts, "dp_relative_bias_grads"), int(bool(bidirectional)), B, H, Tq, Tk, _f32(_dense("grads", grads)))
     _check(ctx, st, "dp_relative_bias_grads")
 
 
@@ -561,6 +578,7 @@ def _qk(q, k, gain_q, gain_k, cos, sin, positions, dense, strided):
     if positions is not None and tuple(positions.shape) != (B, T):
         raise ValueError(f"positions of shape {tuple(positions.shape)}: ({B}, {T}) expected")
     _where(q, k, gain_q, gain_k, cos, sin, positions, *(x[1] for x in dense), *(x[1] for x in strided))
+    _ints("queries and keys", B, T, Hq, Hk, D, n_pos, R)
     head = (q.data_ptr(), k.data_ptr(), _dtype_of(q), ldq, ldk, _f32(_dense("gain_q", gain_q)), _f32(_dense("gain_k", gain_k)), _f32(cos), _f32(sin), n_pos,
             _i32(None if positions is None else _dense("positions", positions)))
     return head, (B, T, Hq, Hk, D, R)

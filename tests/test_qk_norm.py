@@ -325,3 +325,25 @@ def test_examples_of_more_than_a_billion_tokens_are_not_refused():
         args = (at(1), None, pkg.DP_BF16, 8, 8, at(2), None, None, None, 0, None, 0, 1, T, 1, 0, 8, 0, 1e-6)
         assert lib.dp_qk_norm(ctx, *args, at(3), None) == -8, T
         assert lib.dp_qk_norm_grads(ctx, *args, at(4), None, at(5), at(6), None) == -8, T
+
+
+def test_sizes_beyond_32_bits_are_refused():
+    """... and not cut down to what is left of them."""
+    import paper_2108_01624_amd as pkg
+
+    if torch.cuda.is_available():
+        pytest.skip("on the CPU, where no call could touch memory")
+    pkg.load_library()
+    block = ctypes.create_string_buffer(1 << 14)
+    ctx = object.__new__(pkg.Context)
+    ctx.handle = ctypes.addressof(block)
+    long, z = (1 << 32) + 1, torch.zeros
+    g, x = z(16), z(2, 3, 1, 16)
+    for call in (lambda: ctx.qk_norm(z(0, long, 1, 16), z(0, long, 1, 16), g, g, None, None, z(0, long, 1, 16), z(0, long, 1, 16)),
+                 lambda: ctx.qk_norm_grads(z(long, 0, 1, 16), z(long, 0, 1, 16), g, g, None, None, z(long, 0, 1, 16), z(long, 0, 1, 16),
+                                           z(1).expand(long, 2, 16)),
+                 lambda: ctx.qk_norm(x, x, g, g, z(long, 0), z(long, 0), z(2, 3, 1, 16), z(2, 3, 1, 16))):
+        with pytest.raises(pkg.DpError) as e:
+            call()
+        assert e.value.status == -2
+    ctx.handle = None

@@ -335,3 +335,33 @@ def test_refusals_of_outputs_that_overlap():
     assert grads(at(360), x) == -8 and grads(at(359), x) == -5 and grads(at(120), x) == -5 and grads(at(120), x[::2]) == -8 and grads(at(97), x[1:]) == -5
     assert grads(at(96), x[1:]) == -8 and grads(at(60), x[:1], dt=BF) == -8 and grads(at(59), x[:1], dt=BF) == -5
     assert grads(at(360), x, ln=at(384)) == -8 and grads(at(360), x, ln=at(383)) == -5 and grads(at(360), x, ln=at(359)) == -5 and grads(at(400), x, ln=at(398)) == -8
+
+
+def test_numbers_beyond_32_bits_are_refused():
+    """... and not cut down to what is left of them, in the functions as in the methods of a context (which leave such numbers to the functions)."""
+    import paper_2108_01624_amd as pkg
+
+    if torch.cuda.is_available():
+        pytest.skip("on the CPU, where no call could touch memory")
+    pkg.load_library()
+    for n, reach in ((16, (1 << 32) + 128), (16, 128 - (1 << 32)), ((1 << 32) + 16, 128), (16 - (1 << 32), 128), (-1, 128), (16, 1 << 80)):
+        with pytest.raises(pkg.DpError) as e:
+            pkg.dp_relative_buckets(n, reach)
+        assert e.value.status == -5
+    block = ctypes.create_string_buffer(1 << 14)
+    ctx = object.__new__(pkg.Context)
+    ctx.handle = ctypes.addressof(block)
+    table, bias, dS, grads = torch.zeros(3, 2), torch.zeros(2, 4, 4), torch.zeros(2, 2, 4, 4), torch.zeros(2, 3, 2)
+    for s in ([0, 1, (1 << 32) + 5], [0, 1 - (1 << 32), 5], [1 << 32, 1, 5], [0, 1, 1 << 70], [0, 1, (1 << 30) + 1]):
+        for call in (lambda: pkg.dp_relative_bias(ctx.handle, table, s, False, bias), lambda: ctx.relative_bias(table, s, False, bias),
+                     lambda: pkg.dp_relative_bias_grads(ctx.handle, [dS], s, False, grads), lambda: ctx.relative_bias_grads([dS], s, False, grads)):
+            with pytest.raises(pkg.DpError) as e:
+                call()
+            assert e.value.status == -5
+    table, s, long = torch.zeros(3, 0), [0, 1, 2], (1 << 32) + 8   # (no heads: nothing to allocate)
+    for call in (lambda: ctx.relative_bias(table, s, False, torch.zeros(0, 4, long)), lambda: ctx.relative_bias(table, s, False, torch.zeros(0, long, 4)),
+                 lambda: ctx.relative_bias_grads([torch.zeros(2, 0, 4, long)], s, False, torch.zeros(2, 3, 0))):
+        with pytest.raises(pkg.DpError) as e:
+            call()
+        assert e.value.status == -2
+    ctx.handle = None
