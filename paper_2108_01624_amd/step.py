@@ -19,8 +19,14 @@ _HELD = ("grads", "relative_bias", "qk_norm")
 
 def _examples(layer):
     kind = layer["kind"]
+    if kind == "grads" and not layer["grads"]:
+        raise ValueError("a layer of no gradients: it has no examples")
     t = layer["grads"][0] if kind == "grads" else layer["dS"][0] if kind == "relative_bias" else layer["q"] if kind == "qk_norm" else layer["G"]
     return t.shape[0]
+
+
+def _address(t):
+    return None if t is None else t.data_ptr()
 
 
 class StepRunner:
@@ -32,8 +38,8 @@ class StepRunner:
       "grads"          grads: a list of tensors [B, ...], the examples' gradients of the layer's tensors, as the caller's backward holds them
       "relative_bias"  dS: the list of score gradients of the layers that share the table, starts, bidirectional; lengths, causal if there are any
       "qk_norm"        q, k, gain_q, gain_k, cos, sin, dyq, dyk; positions, interleaved, eps, and dq, dk to be written, if there are any
-    (the tensors of "relative_bias" are the table, those of "qk_norm" the two gains).  pass2 uses the gradients of the last two that pass1 of the
-    same micro-batch has left."""
+    (the tensors of "relative_bias" are the table, those of "qk_norm" the two gains).  pass2 uses
+    the gradients of the last two that the last pass1 has left, and refuses layers whose tensors or arguments are not those that it was given."""
 
     def __init__(self, ctx, manifest, max_batch, device="cuda:0"):
         import torch
@@ -64,7 +70,7 @@ class StepRunner:
         self.ln_keep = {}
         self._kept_for = None
         self.grad_keep = {}     # ... and the gradients of bias tables and of gains of queries and keys
-        self._grads_of = None   # examples whose gradients these are
+        self._grads_of = None   # identifies the layers whose gradients these are (_held_token)
 
     def view(self, buf, layer, k):
         off, shp = self.offsets[layer][k]
@@ -80,41 +86,78 @@ class StepRunner:
             self.ln_keep[k] = buf
         return buf
 
-    def _grad_buffer(self, k, shape):
-        """[examples, ...] floats for layer k of the manifest, of a buffer for max_batch examples that is allocated on first use."""
-        import torch
+    def _check_held(self, layers, held, nB):
+        """Refuses gradients that are not those of the manifest's tensors, before anything is called or allocated."""
+        for k in held:
+            l, shapes = layers[k], [tuple(shp) for _, shp in self.offsets[k]]
+            if _examples(l) != nB:
+                raise ValueError(f"layer {k}: gradients of {_examples(l)} examples in a micro-batch of {nB}")
+            if l["kind"] == "grads":
+                if len(l["grads"]) != len(shapes):
+                    raise ValueError(f"layer {k}: {len(l['grads'])} gradients for {len(shapes)} tensors")
+                for g, shp in zip(l["grads"], shapes):
+                    if g.dim() == 0 or g.shape[0] != nB:
+                        raise ValueError(f"layer {k}: a gradient of shape {tuple(g.shape)} in a micro-batch of {nB} examples")
+                    if g.numel() != nB * _elements(shp):
+                        raise ValueError(f"layer {k}: gradients of shape {tuple(g.shape[1:])}, which is not that of the manifest's tensor")
+            elif l["kind"] == "relative_bias":
+                table = (len(l["starts"]) * (2 if l["bidirectional"] else 1), l["dS"][0].shape[1])
+                if shapes != [table]:
+                    raise ValueError(f"layer {k}: a table of shape {table}, the manifest has {shapes}")
+            else:
+                d = l["q"].shape[3]
+                if shapes != [(d,), (d,)]:
+                    raise ValueError(f"layer {k}: gains of shape ({d},) expected, the manifest has {shapes}")
 
-        n = _elements(shape[1:])
-        buf = self.grad_keep.get(k)
-        if buf is None or buf.numel() < self.max_batch * n:
-            buf = self.grad_keep[k] = torch.empty(self.max_batch * n, dtype=torch.float32, device=self.device)
-        return buf[:shape[0] * n].view(*shape)
+    @staticmethod
+    def _held_token(layers, held, nB):
+        """Identifies the layers whose gradients the buffers hold: what their calls read, by address, and every argument that decides the result."""
+        token = [nB]
+        for k in held:
+            l = layers[k]
+            if l["kind"] == "relative_bias":
+                token.append((k, [(x.data_ptr(), x.shape, x.dtype) for x in l["dS"]], list(l["starts"]), bool(l["bidirectional"]), _address(l.get("lengths")),
+                              bool(l.get("causal", False))))
+            elif l["kind"] == "qk_norm":
+                token.append((k, [(l[n].data_ptr(), l[n].shape, l[n].stride(), l[n].dtype) for n in ("q", "k", "dyq", "dyk")],
+                              [_address(l.get(n)) for n in ("cos", "sin", "positions")], bool(l.get("interleaved", False)), float(l.get("eps", 1e-6))))
+        return token
 
     def _held_pass1(self, layers, held, nB, n):
         """Gradients of the bias tables and gains, and the norms of all gradients that exist as tensors."""
-        self._grads_of = self._kept_for = None
+        import torch
+
+        self._kept_for = None
         if any(_examples(l) != nB for l in layers):
             raise ValueError("layers of one micro-batch have as many examples each")
+        self._check_held(layers, held, nB)
+        for k in held:
+            if layers[k]["kind"] != "grads" and k not in self.grad_keep:   # for max_batch examples, of the size that the manifest gives: they stay where they are
+                self.grad_keep[k] = torch.empty(self.max_batch * sum(_elements(shp) for _, shp in self.offsets[k]), dtype=torch.float32, device=self.device)
         groups = self._held_tensors(layers, held, nB)
         for k in held:
             l = layers[k]
             if l["kind"] == "relative_bias":
-                buckets = len(l["starts"]) * (2 if l["bidirectional"] else 1)
-                self.ctx.relative_bias_grads(l["dS"], l["starts"], l["bidirectional"], self._grad_buffer(k, (nB, buckets, l["dS"][0].shape[1])),
-                                             lengths=l.get("lengths"), causal=l.get("causal", False))
+                self.ctx.relative_bias_grads(l["dS"], l["starts"], l["bidirectional"], self._kept_grads(k, nB), lengths=l.get("lengths"), causal=l.get("causal", False))
             elif l["kind"] == "qk_norm":
-                self.ctx.qk_norm_grads(l["q"], l["k"], l["gain_q"], l["gain_k"], l["cos"], l["sin"], l["dyq"], l["dyk"],
-                                       self._grad_buffer(k, (nB, 2, l["q"].shape[3])), l.get("dq"), l.get("dk"), positions=l.get("positions"),
-                                       interleaved=l.get("interleaved", False), eps=l.get("eps", 1e-6))
-        self._grads_of = nB
+                self.ctx.qk_norm_grads(l["q"], l["k"], l["gain_q"], l["gain_k"], l["cos"], l["sin"], l["dyq"], l["dyk"], self._kept_grads(k, nB), l.get("dq"), l.get("dk"),
+                                       positions=l.get("positions"), interleaved=l.get("interleaved", False), eps=l.get("eps", 1e-6))
+        self._grads_of = self._held_token(layers, held, nB)
         for Xs, _ in groups:
             self.ctx.sqnorms_grads(Xs, n)
 
     def _held_pass2(self, layers, held, nB, C, n):
-        if self._grads_of != nB and any(layers[k]["kind"] != "grads" for k in held):
+        self._check_held(layers, held, nB)
+        if self._grads_of != self._held_token(layers, held, nB) and any(layers[k]["kind"] != "grads" for k in held):
             raise ValueError("pass1 of this micro-batch first: it leaves the gradients that are summed here")
         for Xs, sums in self._held_tensors(layers, held, nB):
             self.ctx.clip_accumulate_grads(Xs, C, n, sums)
+
+    def _kept_grads(self, k, nB):
+        """The gradients of layer k that pass 1 leaves: [examples, buckets, heads], [examples, 2, width of a head]."""
+        shapes = [tuple(shp) for _, shp in self.offsets[k]]
+        shape = (nB,) + (shapes[0] if len(shapes) == 1 else (2,) + shapes[0])
+        return self.grad_keep[k][:_elements(shape)].view(shape)
 
     def _held_tensors(self, layers, held, nB):
         """[(gradients, their sums)] of one type each."""
@@ -122,22 +165,13 @@ class StepRunner:
         for k in held:
             l = layers[k]
             if l["kind"] == "grads":
-                if len(l["grads"]) != len(self.offsets[k]):
-                    raise ValueError(f"layer {k}: {len(l['grads'])} gradients for {len(self.offsets[k])} tensors")
                 pairs = [(g, self.view(self.S, k, j)) for j, g in enumerate(l["grads"])]
             elif l["kind"] == "relative_bias":
-                n = len(l["starts"]) * (2 if l["bidirectional"] else 1)
-                pairs = [(self._grad_buffer(k, (nB, n, l["dS"][0].shape[1])), self.view(self.S, k, 0))]
+                pairs = [(self._kept_grads(k, nB), self.view(self.S, k, 0))]
             else:   # the gains' sums lie next to each other: heads are a multiple of 8 wide, tensors start at multiples of 4 floats
                 off, d = self.offsets[k][0][0], l["q"].shape[3]
-                if [shp for _, shp in self.offsets[k]] != [(d,), (d,)]:
-                    raise ValueError(f"layer {k}: gains of shape ({d},) expected")
-                pairs = [(self._grad_buffer(k, (nB, 2, d)), self.S[off:off + 2 * d])]
+                pairs = [(self._kept_grads(k, nB), self.S[off:off + 2 * d])]
             for g, out in pairs:
-                if g.shape[0] != nB:
-                    raise ValueError(f"layer {k}: gradients of {g.shape[0]} examples in a micro-batch of {nB}")
-                if g.numel() != nB * out.numel():
-                    raise ValueError(f"layer {k}: gradients of shape {tuple(g.shape[1:])}, which is not that of the manifest's tensor")
                 xs, sums = by_type.setdefault(g.dtype, ([], []))
                 xs.append(g)
                 sums.append(out)
@@ -184,6 +218,7 @@ class StepRunner:
         micro-batch is over on the GPU before Python has looked at 96 tensors twice)."""
         ctx = self.ctx
         nB, n = self._norms(layers)
+        self._grads_of = None   # (of whatever the norms were that are cleared now)
         ctx.zero_f32(n)
         layers_all = layers
         layers, _, held = self._split(layers)

@@ -319,5 +319,93 @@ def test_calls_of_a_step_with_held_layers(tmp_path):
     assert r.returncode == 0, (r.stdout + r.stderr)[-8000:]
 
 
+def kept_gradients_are_those_of_pass_1():
+    """(in a process on the stub of test_step_calls) pass 2 takes the gradients that pass 1 left for these very layers, or refuses."""
+    from test_step_calls import _package
+
+    pkg, context, lines = _package()
+    s = dict(SIZES, B=4)
+    specs = manifest(s["d"], s["H"], s["D"], s["V"])
+    run = pkg.StepRunner(context(), specs, 4, device="cpu")
+    first, second = (micro_batch(**s, seed=k, device="cpu") for k in (1, 2))
+
+    def refused(call, layers):
+        lines()
+        try:
+            call(layers)
+        except ValueError:
+            assert not [x for x in lines() if "clip_accumulate" in x]
+            return
+        raise AssertionError("not refused")
+
+    two = lambda layers: run.pass2(layers, 1.0)
+    run.pass1(first)
+    two(first)
+    two(first)                                             # (again, say with another clip norm)
+    two([dict(l) for l in first])                          # the same tensors in other dicts
+    refused(two, second)                                   # another micro-batch of as many examples
+    run.pass1(second)
+    refused(two, first)
+    two(second)
+    buffers = {k: b.data_ptr() for k, b in run.grad_keep.items()}
+    change = lambda k, **c: [dict(l, **c) if j == k else l for j, l in enumerate(second)]
+    bias, qk = second[1], second[3]
+    for k, c in ((1, dict(dS=bias["dS"][::-1])), (1, dict(dS=bias["dS"][:1])), (1, dict(lengths=None)), (1, dict(causal=True)), (1, dict(lengths=bias["lengths"].clone())),
+                 (1, dict(starts=[0] + bias["starts"][:-1])), (3, dict(eps=1e-3)), (3, dict(interleaved=True)), (3, dict(cos=qk["sin"])), (3, dict(cos=None, sin=None)),
+                 (3, dict(positions=torch.zeros(4, s["T"], dtype=torch.int32))), (3, dict(q=qk["k"])), (3, dict(dyk=qk["dyq"])),
+                 (3, dict(q=qk["q"].contiguous()))):
+        refused(two, change(k, **c))
+    two(second)
+    two(change(5, grads=[t.clone() for t in second[5]["grads"]]))   # what the caller holds is read from where it is
+    # layers that are refused leave the gradients and the places of their buffers alone (a captured graph writes there)
+    larger = [dict(starts=list(range(9))), dict(bidirectional=False), dict(dS=[torch.zeros(4, s["H"] + 1, s["T"], s["T"])] * 2)]
+    for c in larger:
+        refused(two, change(1, **c))
+        two(second)
+    for c in larger:
+        refused(run.pass1, change(1, **c))
+    run.pass1(second)
+    two(second)
+    assert buffers == {k: b.data_ptr() for k, b in run.grad_keep.items()}
+    # after a pass 1 without such layers there is nothing to be taken
+    dense = [second[2]]
+    run.pass1(dense)
+    refused(two, second)
+    # a table of the manifest that the layer has not: refused, where it is too small as well
+    for shapes in (((2 * len(STARTS), s["H"]), (5,)), ((2 * len(STARTS) * s["H"],),), ((s["H"], 2 * len(STARTS)),)):
+        other = pkg.StepRunner(context(), [Spec(*shapes)], 4, device="cpu")
+        refused(other.pass1, [bias])
+        assert not other.grad_keep
+    other = pkg.StepRunner(context(), [Spec((5,))], 4, device="cpu")
+    refused(other.pass1, [dict(kind="grads", grads=[])])
+
+
+def _on_the_stub(tmp_path, name):
+    """Runs the function of that name, above, in a process whose package stands on the stub."""
+    import shutil
+
+    from paper_2108_01624_amd import build
+    from test_step_calls import PKG, _stub_source
+
+    (tmp_path / PKG).mkdir()
+    for f in os.listdir(build.PKG_DIR):
+        if f.endswith(".py"):
+            shutil.copy(os.path.join(build.PKG_DIR, f), tmp_path / PKG / f)
+    shutil.copy(build.NATIVE_PATH, tmp_path / PKG / "_native.so")
+    (tmp_path / "stub.cpp").write_text(_stub_source())
+    r = subprocess.run(["g++", "-shared", "-fPIC", "-O1", "-std=c++17", "-I" + build.INCLUDE, "-Wl,-soname,libdpclip.so", str(tmp_path / "stub.cpp"),
+                        "-o", str(tmp_path / PKG / "libdpclip.so")], capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-3000:]
+    r = subprocess.run([sys.executable, os.path.abspath(__file__), name], capture_output=True, text=True, cwd=tmp_path, timeout=600,
+                       env=dict(os.environ, PYTHONPATH=str(tmp_path)))
+    assert r.returncode == 0, (r.stdout + r.stderr)[-8000:]
+
+
+def test_kept_gradients_are_those_of_pass_1(tmp_path):
+    if torch.cuda.is_available():
+        pytest.skip("tensors of the CPU beside a stub: where there is no GPU")
+    _on_the_stub(tmp_path, "kept_gradients_are_those_of_pass_1")
+
+
 if __name__ == "__main__":
     globals()[sys.argv[1]]()
