@@ -74,7 +74,7 @@ class StepRunner:
 
     def view(self, buf, layer, k):
         off, shp = self.offsets[layer][k]
-        return buf[off:off + _elements(shp)].view(*shp)
+        return buf[off:off + _elements(shp)].view(tuple(shp))
 
     def _keep_buffer(self, k, d):
         """[max_batch, 2, d] floats for layer k of the manifest, allocated on first use."""

@@ -380,6 +380,19 @@ def kept_gradients_are_those_of_pass_1():
     refused(other.pass1, [dict(kind="grads", grads=[])])
 
 
+def scalar_parameters():
+    """(in a process on the stub of test_step_calls) a tensor of no axes, next to others."""
+    from test_step_calls import _package
+
+    pkg, context, lines = _package()
+    run = pkg.StepRunner(context(), [Spec((), (3,)), Spec(())], 4, device="cpu")
+    layers = [dict(kind="grads", grads=[torch.zeros(4), torch.zeros(4, 3)]), dict(kind="grads", grads=[torch.zeros(4, 1)])]
+    run.pass1(layers)
+    run.pass2(layers, 1.0)
+    assert [x.split()[0] for x in lines()] == ["dp_zero_f32", "dp_sqnorms_grads", "dp_clip_accumulate_grads"]
+    assert run.view(run.S, 0, 0).shape == () and run.view(run.theta, 0, 1).shape == (3,) and run.P == 9
+
+
 def _on_the_stub(tmp_path, name):
     """Runs the function of that name, above, in a process whose package stands on the stub."""
     import shutil
@@ -405,6 +418,12 @@ def test_kept_gradients_are_those_of_pass_1(tmp_path):
     if torch.cuda.is_available():
         pytest.skip("tensors of the CPU beside a stub: where there is no GPU")
     _on_the_stub(tmp_path, "kept_gradients_are_those_of_pass_1")
+
+
+def test_scalar_parameters(tmp_path):
+    if torch.cuda.is_available():
+        pytest.skip("tensors of the CPU beside a stub: where there is no GPU")
+    _on_the_stub(tmp_path, "scalar_parameters")
 
 
 if __name__ == "__main__":
