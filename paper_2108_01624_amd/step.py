@@ -19,8 +19,8 @@ _HELD = ("grads", "relative_bias", "qk_norm")
 
 def _examples(layer):
     kind = layer["kind"]
-    if kind == "grads" and not layer["grads"]:
-        raise ValueError("a layer of no gradients: it has no examples")
+    if kind == "grads" and (not layer["grads"] or layer["grads"][0].dim() == 0):
+        raise ValueError("a layer of no gradients, or of one that has no examples")
     t = layer["grads"][0] if kind == "grads" else layer["dS"][0] if kind == "relative_bias" else layer["q"] if kind == "qk_norm" else layer["G"]
     return t.shape[0]
 
@@ -38,7 +38,7 @@ class StepRunner:
       "grads"          grads: a list of tensors [B, ...], the examples' gradients of the layer's tensors, as the caller's backward holds them
       "relative_bias"  dS: the list of score gradients of the layers that share the table, starts, bidirectional; lengths, causal if there are any
       "qk_norm"        q, k, gain_q, gain_k, cos, sin, dyq, dyk; positions, interleaved, eps, and dq, dk to be written, if there are any
-    (the tensors of "relative_bias" are the table, those of "qk_norm" the two gains).  pass2 uses
+    (the tensors of "relative_bias" are the table, those of "qk_norm" the two gains; gradients have the shape of their tensor, or are flat).  pass2 uses
     the gradients of the last two that the last pass1 has left, and refuses layers whose tensors or arguments are not those that it was given."""
 
     def __init__(self, ctx, manifest, max_batch, device="cuda:0"):
@@ -98,8 +98,9 @@ class StepRunner:
                 for g, shp in zip(l["grads"], shapes):
                     if g.dim() == 0 or g.shape[0] != nB:
                         raise ValueError(f"layer {k}: a gradient of shape {tuple(g.shape)} in a micro-batch of {nB} examples")
-                    if g.numel() != nB * _elements(shp):
-                        raise ValueError(f"layer {k}: gradients of shape {tuple(g.shape[1:])}, which is not that of the manifest's tensor")
+                    long = lambda sizes: [n for n in sizes if n != 1]   # (axes of one do not change the order of the numbers)
+                    if long(g.shape[1:]) != long(shp) and tuple(g.shape[1:]) != (_elements(shp),):
+                        raise ValueError(f"layer {k}: gradients of shape {tuple(g.shape[1:])}, which is not that of the manifest's tensor, {shp}")
             elif l["kind"] == "relative_bias":
                 table = (len(l["starts"]) * (2 if l["bidirectional"] else 1), l["dS"][0].shape[1])
                 if shapes != [table]:

@@ -380,6 +380,30 @@ def kept_gradients_are_those_of_pass_1():
     refused(other.pass1, [dict(kind="grads", grads=[])])
 
 
+def shapes_of_held_gradients():
+    """(in a process on the stub of test_step_calls) gradients have the shape of the manifest's tensor, up to axes of one, or are flat."""
+    from test_step_calls import _package
+
+    pkg, context, lines = _package()
+    run = pkg.StepRunner(context(), [Spec((6, 3), (4, 1, 5), ())], 4, device="cpu")
+    z = torch.zeros
+    good = ((4, 6, 3), (4, 4, 1, 5), (4,))
+    for change in ((), (0, (4, 18)), (0, (4, 6, 1, 3)), (1, (4, 4, 5)), (1, (4, 20)), (2, (4, 1))):
+        grads = [z(change[1] if change and change[0] == k else s) for k, s in enumerate(good)]
+        run.pass1([dict(kind="grads", grads=grads)])
+        run.pass2([dict(kind="grads", grads=grads)], 1.0)
+        assert [x.split()[0] for x in lines()] == ["dp_zero_f32", "dp_sqnorms_grads", "dp_clip_accumulate_grads"]
+    for k, shape in ((0, (4, 3, 6)), (0, (4, 2, 9)), (0, (4, 6, 2)), (0, (4, 17)), (1, (4, 5, 4)), (1, (4, 5, 1, 4)), (1, (4, 2, 2, 5)), (2, (4, 2)), (2, ()), (0, ()), (0, (3, 6, 3)), (1, (5, 4, 1, 5))):
+        grads = [z(shape if j == k else s) for j, s in enumerate(good)]
+        for call in (run.pass1, lambda layers: run.pass2(layers, 1.0)):
+            try:
+                call([dict(kind="grads", grads=grads)])
+            except ValueError:
+                assert all(x.split()[0] == "dp_zero_f32" for x in lines())
+                continue
+            raise AssertionError(f"not refused: {shape}")
+
+
 def scalar_parameters():
     """(in a process on the stub of test_step_calls) a tensor of no axes, next to others."""
     from test_step_calls import _package
@@ -424,6 +448,12 @@ def test_scalar_parameters(tmp_path):
     if torch.cuda.is_available():
         pytest.skip("tensors of the CPU beside a stub: where there is no GPU")
     _on_the_stub(tmp_path, "scalar_parameters")
+
+
+def test_shapes_of_held_gradients(tmp_path):
+    if torch.cuda.is_available():
+        pytest.skip("tensors of the CPU beside a stub: where there is no GPU")
+    _on_the_stub(tmp_path, "shapes_of_held_gradients")
 
 
 if __name__ == "__main__":
