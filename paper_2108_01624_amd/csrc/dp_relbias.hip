@@ -120,6 +120,8 @@ __device__ __forceinline__ RelPlan rel_plan(int layers, int rows, int cols, int 
 }
 
 constexpr int SUMS = 15;  // diagonals of a block of 8 x 8
+constexpr size_t MOST_LDS = (2 * SUMS * 256 + DP_REL_MAX_LINE) * sizeof(float);  // sums of 256 threads, and all diagonals
+static_assert(MOST_LDS + 256 <= 160 * 1024, "the diagonals of a plane lie in a CU's local memory");
 
 // part[i][bucket][h] (or, with several parts, part[slot][...]) = sums of the buckets.
 //
@@ -405,8 +407,8 @@ dp_status dpk_relbias_grads(dp_ctx* ctx, int n_layers, const void* const* dS, dp
         const dim3 grid((unsigned)(planes * splits));
         const int slot0 = l0 / REL_LAYERS * splits;
         auto launch = [&](auto kernel) {
-            // (what this launch takes, 158 KiB at most: with the kernel's static words a request for all 160 KiB of a CU is refused)
-            if (lds > 65536) DP_HIP_CHECK(ctx, hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds));
+            // (always the most that a launch can take, as contexts of several threads share the kernel; not a CU's 160 KiB, of which its static words are a part)
+            if (lds > 65536) DP_HIP_CHECK(ctx, hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)MOST_LDS));
             hipLaunchKernelGGL(kernel, grid, dim3(threads), lds, ctx->stream, t, bk, lengths, causal, splits, near_lo, near_hi, B, H, Tq, Tk, part, slot0);
             return DP_OK;
         };

@@ -365,3 +365,58 @@ def test_numbers_beyond_32_bits_are_refused():
             call()
         assert e.value.status == -2
     ctx.handle = None
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Tq,Tk", [(700, 700), (333, 1500), (1, 5000)])
+@pytest.mark.parametrize("causal", [False, True])
+def test_grads_of_a_padded_batch_of_long_examples(dp, dtype, Tq, Tk, causal):
+    """Planes that several workgroups share, of which short examples leave some without work; NaN and infinities in every place that does not count."""
+    lengths = torch.tensor([Tk, 0, Tk - 3, Tk // 2 + 1, Tk - Tq, Tk - Tq + 1], dtype=torch.int32)
+    B, H = len(lengths), 2
+    dS = _scores(3, B, H, Tq, Tk, dtype, Tk)
+    pos, key, n = torch.arange(Tq) + Tk - Tq, torch.arange(Tk), lengths[:, None, None]
+    out = ~((pos[None, :, None] < n) & (key[None, None, :] < n))[:, None].expand(B, H, Tq, Tk)
+    if causal:
+        out = out | (_rel(Tq, Tk) > 0)
+    for x, v in zip(dS, (float("nan"), float("inf"), -float("inf"))):
+        x[out.to(DEV)] = v
+    for s, both in ((STARTS["t16"], True), ([0, 2, 30, 600], True), (STARTS["n128"], False)):
+        grads = torch.full((B, len(s) * (2 if both else 1), H), 5.0, device=DEV)
+        dp.relative_bias_grads(dS, s, both, grads, lengths=lengths.to(DEV), causal=causal)
+        dp.sync()
+        _check_sums(grads, dS, s, both, lengths, causal)
+
+
+@pytest.mark.gpu
+def test_grads_of_long_lines_replay_from_a_graph():
+    """More local memory than a launch has without asking: the request may be made while a graph is recorded."""
+    import paper_2108_01624_amd as pkg
+
+    s = [0, 1, 30, 11000]
+    x = [_scores(1, 2, 1, 5, 12000, "bf16", k)[0] for k in range(3)]
+    side = torch.cuda.Stream(device=DEV)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        ctx = pkg.Context()
+        dS, grads = x[0].clone(), torch.empty(2, 8, 1, device=DEV)
+        graph = torch.cuda.CUDAGraph()
+        side.synchronize()
+        with torch.cuda.graph(graph, stream=side):
+            ctx.relative_bias_grads([dS], s, True, grads)
+    for k in (1, 0, 2, 2):
+        with torch.cuda.stream(side):
+            dS.copy_(x[k])
+            grads.fill_(7)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        ctx.sync()
+        _check_sums(grads, [x[k]], s, True, None, False)
+        eager = torch.empty_like(grads)
+        ctx.relative_bias_grads([x[k]], s, True, eager)
+        ctx.sync()
+        assert torch.equal(eager, grads)
+    del graph
+    ctx.close()
