@@ -5,8 +5,8 @@
 // entry of the sums; the scaled form reads and writes it.  Rows start wherever n_l puts them: wide accesses are declared with the
 // alignment of an element, which the hardware serves at any address.
 //
-// 334 M bf16 elements of 388 tensors, one unit: norms 109 us in three launches (6.1 TB/s), sums 556 us (6.0 TB/s of reading and writing);
-// 128 units of 96 tensors of 8,192 bf16 elements: norms 34 us (6.0 TB/s), sums 42; 41 M fp32 elements scaled: 56 us (5.9 TB/s).
+// 334 M bf16 elements of 388 tensors, one unit: norms 112 us in three launches and their join (6.0 TB/s), sums 558 us (6.0 TB/s of reading and writing);
+// 128 units of 96 tensors of 8,192 bf16 elements: norms 34 us (6.0 TB/s), sums 41; 41 M fp32 elements scaled: 56 us (5.9 TB/s).
 #include "dp_common.h"
 
 namespace {
@@ -14,10 +14,10 @@ namespace {
 constexpr int HELD_TABLE = 160;          // tensors per launch: their table is a kernel argument, of less than 4 KiB
 constexpr int HELD_FEW = 32;             // a small table where it is enough (16 tensors: a call of the sums 4.7 -> 3.8 us of host time)
 constexpr uint64_t HELD_ENTRY = 1ull << 31;  // most elements of an entry (32-bit counters have room behind them); one unit's longer tensors are several entries
-constexpr uint64_t HELD_PIECE = 16384;   // elements of a workgroup of the norms (334 M bf16: 98 us; 4,096: 101, 65,536: 102)
+constexpr uint64_t HELD_PIECE = 16384;   // elements of a workgroup of the norms (334 M bf16 in 388 tensors: 112 us; 4,096: 144, 65,536: 114)
 constexpr int WAVE_ROW = 4096;           // rows up to this length are one wave's (256 units of 96 rows of 2,048 bf16: 45 us norms and sums; up to 1,024: 59)
 constexpr unsigned ADD_GRID = 256;       // most workgroups, and units, of a launch of norms whose last workgroup adds them up (16 tensors of a small
-                                         // block: a pass of 13.5 us, with a launch for it 18.9)
+                                         // block: a launch behind them costs a pass 5 us more)
 constexpr int ADD_UNITS = 16;
 constexpr int ADD_COLS = 256 * 4;        // columns of a workgroup of the sums, one unit
 constexpr int SUM_COLS = 64 * 8;         // ... several units
@@ -31,8 +31,8 @@ typedef u32x2_t u32x2_a2 __attribute__((aligned(2)));
 typedef f32x4_t f32x4_a4 __attribute__((aligned(4)));
 
 // Elements from any address of an element.  STREAM: with the non-temporal hint.  The second pass and the sums carry it; the norms do where the
-// gradients are more than the last-level cache keeps for the second pass (164 MB fp32, norms and scaling: 97 us with cached norms, 107 with
-// streamed ones; 668 MB bf16 streamed, norms alone: 98 us, cached 110).
+// gradients are more than the last-level cache keeps for the second pass (164 MB fp32, norms and scaling: 87 us with cached norms, 97 with
+// streamed ones; 668 MB bf16 streamed, norms alone: 112 us, cached 124).
 template <bool BF16, bool STREAM = true>
 struct Held {
     typedef typename std::conditional<BF16, uint16_t, float>::type elem;
@@ -109,8 +109,8 @@ void with_table(const HeldFull& t, Launch launch) {
     launch(few);
 }
 
-// The tensor of workgroup b: a search by halves over scalar loads.  (Two entries a lane and ballots, one round of vector loads, cost a
-// workgroup of 1,024 columns more than its work: 334 M bf16 elements added to their sums 684 us that way, 503 this way.)
+// The tensor of workgroup b: a search by halves over scalar loads.  (Three entries a lane and ballots, one round of vector loads: 334 M bf16 elements
+// added to their sums 555 us, 558 this way.)
 template <int N>
 __device__ __forceinline__ int held_tensor(const HeldTable<N>& t, uint32_t b) {
     int lo = 0, hi = t.n;
@@ -235,7 +235,7 @@ __device__ __forceinline__ float held_factor(const float* sqnorms, int i, float 
 }
 
 // sums[k] += c x[k], one unit.  Four elements a thread, the sums' access the wide one, neighbouring workgroups on neighbouring
-// memory: 334 M bf16 elements 504 us (6.6 TB/s); eight elements a thread 604, two or four times four 548 and 565.
+// memory: 334 M bf16 elements 558 us (6.0 TB/s); eight neighbouring elements a thread 608; two and four groups of four, 1,024 apart, 535 and 546.
 template <bool BF16, int N>
 __global__ __launch_bounds__(256) void held_add_kernel(HeldTable<N> t, float C, const float* __restrict__ sqnorms, int* __restrict__ err) {
     typedef Held<BF16> IO;

@@ -5,7 +5,7 @@
 // that moves by one from row to row.  Gradient: the sums of the diagonals, then those of the buckets' runs.
 //
 // Roofline: HBM, both.  The forward writes H Tq Tk elements, the gradient reads L B H Tq Tk of them with one addition each.
-// Forward, 16 x 2,048 x 2,048: bf16 25 us (5.3 TB/s), fp32 42 us (6.4); gradient, 24 layers x 128 x 16 x 128 x 128 bf16: 240 us (6.7 TB/s),
+// Forward, 16 x 2,048 x 2,048: bf16 23 us (5.8 TB/s; 28 where the buffer is another from call to call), fp32 42 us (6.4); gradient, 24 layers x 128 x 16 x 128 x 128 bf16: 240 us (6.7 TB/s),
 // 12 layers x 64 x 16 x 125 x 125: 72 us (5.3).
 #include "dp_common.h"
 
@@ -369,10 +369,11 @@ dp_status dpk_relbias_grads(dp_ctx* ctx, int n_layers, const void* const* dS, dp
     const bool fold = causal && Tq == Tk;
     const int steps = fold ? (Tq + 15) / 16 : (Tq + 7) / 8;
     if (lengths) {
-        // Short examples leave the last workgroups of their planes empty.  Up to 8,192 where a thread then still has two of its plane's steps, so that
-        // the longest examples are not what all wait for (2 layers of 128 x 12 of up to 509 tokens, causal: 171 -> 155 us); and an odd number, so that
-        // the same part of a plane does not always come to the same XCD (2 layers of 16 x 16 x 1,024, causal: 128 us with 8, 112 with 9; 8 where
+        // Short examples leave the last workgroups of their planes empty.  Up to 8,192 where a thread then still has about two of its plane's steps, so that
+        // the longest examples are not what all wait for (2 layers of 128 x 12 of up to 509 tokens, causal: 171 -> 155 us); and rounded up to an odd number,
+        // so that the same part of a plane does not always come to the same XCD (2 layers of 16 x 16 x 1,024, causal: 128 us with 8, 112 with 9; 8 where
         // 7 had been, 6 layers of 24 x 12 x 509: 160 -> 211.  Planes in the inner order, which any number allows: 104 us instead of 94 under its mask).
+        // A chain of four steps is thereby cut into three parts, and loses: 2 layers of 256 x 16 x 256 without a mask, bf16: 113 -> 121 us.
         const long across = (Tk + 7) / 8 + (fold ? 1 : 0), chain = steps / (across < 256 ? 256 / across : 1);
         const long more = chain / 2 < 8192 / planes ? chain / 2 : 8192 / planes;
         splits = (more > splits ? (int)more : splits) | 1;
