@@ -25,6 +25,24 @@ def _examples(layer):
     return t.shape[0]
 
 
+def _table(layer):
+    """The shape of a relative position bias's table: buckets and heads."""
+    return len(layer["starts"]) * (2 if layer["bidirectional"] else 1), layer["dS"][0].shape[1]
+
+
+def _same_order(a, b):
+    """Whether the numbers of tensors of these shapes stand in one order: one of them is the other with neighbouring axes as one (or is flat)."""
+    def runs(shape):   # numbers from one step of an axis to the next
+        n, out = 1, set()
+        for s in reversed(shape):
+            n *= s
+            out.add(n)
+        return out - {1}
+
+    x, y = runs(a), runs(b)
+    return _elements(a) == _elements(b) and (x <= y or y <= x)
+
+
 def _address(t):
     return None if t is None else t.data_ptr()
 
@@ -38,8 +56,9 @@ class StepRunner:
       "grads"          grads: a list of tensors [B, ...], the examples' gradients of the layer's tensors, as the caller's backward holds them
       "relative_bias"  dS: the list of score gradients of the layers that share the table, starts, bidirectional; lengths, causal if there are any
       "qk_norm"        q, k, gain_q, gain_k, cos, sin, dyq, dyk; positions, interleaved, eps, and dq, dk to be written, if there are any
-    (the tensors of "relative_bias" are the table, those of "qk_norm" the two gains; gradients have the shape of their tensor, or are flat).  pass2 uses
-    the gradients of the last two that the last pass1 has left, and refuses layers whose tensors or arguments are not those that it was given."""
+    (the tensors of "relative_bias" are the table, those of "qk_norm" the two gains; gradients have the shape of their tensor, but that neighbouring axes
+    of either may be one axis of the other).  pass2 uses the gradients of the last two that the last pass1 has left, and refuses layers whose tensors or
+    arguments are not those that it was given."""
 
     def __init__(self, ctx, manifest, max_batch, device="cuda:0"):
         import torch
@@ -96,14 +115,14 @@ class StepRunner:
                 if len(l["grads"]) != len(shapes):
                     raise ValueError(f"layer {k}: {len(l['grads'])} gradients for {len(shapes)} tensors")
                 for g, shp in zip(l["grads"], shapes):
-                    if g.dim() == 0 or g.shape[0] != nB:
-                        raise ValueError(f"layer {k}: a gradient of shape {tuple(g.shape)} in a micro-batch of {nB} examples")
-                    long = lambda sizes: [n for n in sizes if n != 1]   # (axes of one do not change the order of the numbers)
-                    if long(g.shape[1:]) != long(shp) and tuple(g.shape[1:]) != (_elements(shp),):
-                        raise ValueError(f"layer {k}: gradients of shape {tuple(g.shape[1:])}, which is not that of the manifest's tensor, {shp}")
+                    size = g.shape
+                    if not size or size[0] != nB:
+                        raise ValueError(f"layer {k}: a gradient of shape {tuple(size)} in a micro-batch of {nB} examples")
+                    if size[1:] != shp and not _same_order(size[1:], shp):
+                        raise ValueError(f"layer {k}: gradients of shape {tuple(size[1:])}, which is not that of the manifest's tensor, {shp}")
             elif l["kind"] == "relative_bias":
-                table = (len(l["starts"]) * (2 if l["bidirectional"] else 1), l["dS"][0].shape[1])
-                if shapes != [table]:
+                table = _table(l)
+                if len(shapes) != 1 or not _same_order(table, shapes[0]):
                     raise ValueError(f"layer {k}: a table of shape {table}, the manifest has {shapes}")
             else:
                 d = l["q"].shape[3]
@@ -139,9 +158,9 @@ class StepRunner:
         for k in held:
             l = layers[k]
             if l["kind"] == "relative_bias":
-                self.ctx.relative_bias_grads(l["dS"], l["starts"], l["bidirectional"], self._kept_grads(k, nB), lengths=l.get("lengths"), causal=l.get("causal", False))
+                self.ctx.relative_bias_grads(l["dS"], l["starts"], l["bidirectional"], self._kept_grads(k, nB, _table(l)), lengths=l.get("lengths"), causal=l.get("causal", False))
             elif l["kind"] == "qk_norm":
-                self.ctx.qk_norm_grads(l["q"], l["k"], l["gain_q"], l["gain_k"], l["cos"], l["sin"], l["dyq"], l["dyk"], self._kept_grads(k, nB), l.get("dq"), l.get("dk"),
+                self.ctx.qk_norm_grads(l["q"], l["k"], l["gain_q"], l["gain_k"], l["cos"], l["sin"], l["dyq"], l["dyk"], self._kept_grads(k, nB, (2, l["q"].shape[3])), l.get("dq"), l.get("dk"),
                                        positions=l.get("positions"), interleaved=l.get("interleaved", False), eps=l.get("eps", 1e-6))
         self._grads_of = self._held_token(layers, held, nB)
         for Xs, _ in groups:
@@ -154,11 +173,9 @@ class StepRunner:
         for Xs, sums in self._held_tensors(layers, held, nB):
             self.ctx.clip_accumulate_grads(Xs, C, n, sums)
 
-    def _kept_grads(self, k, nB):
-        """The gradients of layer k that pass 1 leaves: [examples, buckets, heads], [examples, 2, width of a head]."""
-        shapes = [tuple(shp) for _, shp in self.offsets[k]]
-        shape = (nB,) + (shapes[0] if len(shapes) == 1 else (2,) + shapes[0])
-        return self.grad_keep[k][:_elements(shape)].view(shape)
+    def _kept_grads(self, k, nB, shape):
+        """The gradients of layer k that pass 1 leaves, of that shape for an example."""
+        return self.grad_keep[k][:nB * _elements(shape)].view(nB, *shape)
 
     def _held_tensors(self, layers, held, nB):
         """[(gradients, their sums)] of one type each."""
@@ -168,10 +185,10 @@ class StepRunner:
             if l["kind"] == "grads":
                 pairs = [(g, self.view(self.S, k, j)) for j, g in enumerate(l["grads"])]
             elif l["kind"] == "relative_bias":
-                pairs = [(self._kept_grads(k, nB), self.view(self.S, k, 0))]
+                pairs = [(self._kept_grads(k, nB, _table(l)), self.view(self.S, k, 0))]
             else:   # the gains' sums lie next to each other: heads are a multiple of 8 wide, tensors start at multiples of 4 floats
                 off, d = self.offsets[k][0][0], l["q"].shape[3]
-                pairs = [(self._kept_grads(k, nB), self.S[off:off + 2 * d])]
+                pairs = [(self._kept_grads(k, nB, (2, d)), self.S[off:off + 2 * d])]
             for g, out in pairs:
                 xs, sums = by_type.setdefault(g.dtype, ([], []))
                 xs.append(g)

@@ -372,7 +372,7 @@ def kept_gradients_are_those_of_pass_1():
     run.pass1(dense)
     refused(two, second)
     # a table of the manifest that the layer has not: refused, where it is too small as well
-    for shapes in (((2 * len(STARTS), s["H"]), (5,)), ((2 * len(STARTS) * s["H"],),), ((s["H"], 2 * len(STARTS)),)):
+    for shapes in (((2 * len(STARTS), s["H"]), (5,)), ((2 * len(STARTS) * s["H"] + 1,),), ((s["H"], 2 * len(STARTS)),), ((len(STARTS), s["H"]),)):
         other = pkg.StepRunner(context(), [Spec(*shapes)], 4, device="cpu")
         refused(other.pass1, [bias])
         assert not other.grad_keep
@@ -381,19 +381,19 @@ def kept_gradients_are_those_of_pass_1():
 
 
 def shapes_of_held_gradients():
-    """(in a process on the stub of test_step_calls) gradients have the shape of the manifest's tensor, up to axes of one, or are flat."""
+    """(in a process on the stub of test_step_calls) gradients have the shape of the manifest's tensor, or one with axes split or joined."""
     from test_step_calls import _package
 
     pkg, context, lines = _package()
     run = pkg.StepRunner(context(), [Spec((6, 3), (4, 1, 5), ())], 4, device="cpu")
     z = torch.zeros
     good = ((4, 6, 3), (4, 4, 1, 5), (4,))
-    for change in ((), (0, (4, 18)), (0, (4, 6, 1, 3)), (1, (4, 4, 5)), (1, (4, 20)), (2, (4, 1))):
+    for change in ((), (0, (4, 18)), (0, (4, 6, 1, 3)), (1, (4, 4, 5)), (1, (4, 20)), (1, (4, 2, 2, 5)), (0, (4, 2, 3, 3)), (2, (4, 1))):
         grads = [z(change[1] if change and change[0] == k else s) for k, s in enumerate(good)]
         run.pass1([dict(kind="grads", grads=grads)])
         run.pass2([dict(kind="grads", grads=grads)], 1.0)
         assert [x.split()[0] for x in lines()] == ["dp_zero_f32", "dp_sqnorms_grads", "dp_clip_accumulate_grads"]
-    for k, shape in ((0, (4, 3, 6)), (0, (4, 2, 9)), (0, (4, 6, 2)), (0, (4, 17)), (1, (4, 5, 4)), (1, (4, 5, 1, 4)), (1, (4, 2, 2, 5)), (2, (4, 2)), (2, ()), (0, ()), (0, (3, 6, 3)), (1, (5, 4, 1, 5))):
+    for k, shape in ((0, (4, 3, 6)), (0, (4, 2, 9)), (0, (4, 6, 2)), (0, (4, 17)), (1, (4, 5, 4)), (1, (4, 5, 1, 4)), (1, (4, 2, 10)), (0, (4, 3, 2, 3, 1, 2)), (2, (4, 2)), (2, ()), (0, ()), (0, (3, 6, 3)), (1, (5, 4, 1, 5))):
         grads = [z(shape if j == k else s) for j, s in enumerate(good)]
         for call in (run.pass1, lambda layers: run.pass2(layers, 1.0)):
             try:
@@ -402,6 +402,25 @@ def shapes_of_held_gradients():
                 assert all(x.split()[0] == "dp_zero_f32" for x in lines())
                 continue
             raise AssertionError(f"not refused: {shape}")
+
+
+def flat_tensors_of_the_manifest():
+    """(in a process on the stub of test_step_calls) a manifest that names the numbers of a tensor only: gradients and tables of any shape."""
+    from test_step_calls import _package
+
+    pkg, context, lines = _package()
+    s = dict(SIZES, B=4)
+    layers = micro_batch(**s, seed=1, device="cpu")
+    layers = [layers[1], dict(kind="grads", grads=[torch.zeros(4, 2, 3, 5), torch.zeros(4, 6, 1)])]
+    run = pkg.StepRunner(context(), [Spec((2 * len(STARTS) * s["H"],)), Spec((2, 15), (6,))], 4, device="cpu")
+    run.pass1(layers)
+    run.pass2(layers, 1.0)
+    assert [x.split()[0] for x in lines()] == ["dp_zero_f32", "dp_relative_bias_grads", "dp_sqnorms_grads", "dp_clip_accumulate_grads"]
+    try:
+        run.pass1([layers[0], dict(kind="grads", grads=[torch.zeros(4, 2, 3, 4), torch.zeros(4, 6)])])
+    except ValueError:
+        return
+    raise AssertionError("not refused")
 
 
 def scalar_parameters():
@@ -442,6 +461,12 @@ def test_kept_gradients_are_those_of_pass_1(tmp_path):
     if torch.cuda.is_available():
         pytest.skip("tensors of the CPU beside a stub: where there is no GPU")
     _on_the_stub(tmp_path, "kept_gradients_are_those_of_pass_1")
+
+
+def test_flat_tensors_of_the_manifest(tmp_path):
+    if torch.cuda.is_available():
+        pytest.skip("tensors of the CPU beside a stub: where there is no GPU")
+    _on_the_stub(tmp_path, "flat_tensors_of_the_manifest")
 
 
 def test_scalar_parameters(tmp_path):
