@@ -521,9 +521,10 @@ def dp_relative_bias(ctx, table, starts, bidirectional, bias):
 
 
 def dp_relative_bias_grads(ctx, dSs, starts, bidirectional, grads, *, lengths=None, causal=False):
-    """dSs: one tensor [B, H, Tq, Tk] per layer that uses the table (gradients of the attention scores); grads [B, buckets, H], overwritten;
-    lengths: int32 [B] or None."""
-    n, (B, H, Tq, Tk), dt = len(starts), dSs[0].shape, dSs[0].dtype
+    """dSs: one tensor [B, H, Tq, Tk] per layer that uses the table (gradients of the attention scores; no layers: zeros); grads [B, buckets, H],
+    overwritten; lengths: int32 [B] or None."""
+    n = len(starts)
+    (B, H, Tq, Tk), dt = (dSs[0].shape, dSs[0].dtype) if len(dSs) else ((grads.shape[0], grads.shape[-1], 0, 0), grads.dtype)
     for x in dSs:
         if tuple(x.shape) != (B, H, Tq, Tk) or x.dtype != dt:
             raise ValueError("all layers of a call must share one shape and dtype")

@@ -19,8 +19,10 @@ _HELD = ("grads", "relative_bias", "qk_norm")
 
 def _examples(layer):
     kind = layer["kind"]
-    if kind == "grads" and (not layer["grads"] or layer["grads"][0].dim() == 0):
-        raise ValueError("a layer of no gradients, or of one that has no examples")
+    if kind in ("grads", "relative_bias"):
+        held = layer["grads" if kind == "grads" else "dS"]
+        if not held or held[0].dim() == 0:
+            raise ValueError("a layer of no gradients, or of one that has no examples")
     t = layer["grads"][0] if kind == "grads" else layer["dS"][0] if kind == "relative_bias" else layer["q"] if kind == "qk_norm" else layer["G"]
     return t.shape[0]
 

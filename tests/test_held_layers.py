@@ -378,6 +378,7 @@ def kept_gradients_are_those_of_pass_1():
         assert not other.grad_keep
     other = pkg.StepRunner(context(), [Spec((5,))], 4, device="cpu")
     refused(other.pass1, [dict(kind="grads", grads=[])])
+    refused(other.pass1, [dict(bias, dS=[])])
 
 
 def shapes_of_held_gradients():

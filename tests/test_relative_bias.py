@@ -420,3 +420,20 @@ def test_grads_of_long_lines_replay_from_a_graph():
         assert torch.equal(eager, grads)
     del graph
     ctx.close()
+
+
+@pytest.mark.gpu
+def test_a_table_that_no_layer_uses_has_no_gradient(dp):
+    import paper_2108_01624_amd as pkg
+
+    s = STARTS["t16"]
+    for both in (False, True):
+        for call in (dp.relative_bias_grads, lambda *a: pkg.dp_relative_bias_grads(dp.handle, *a)):
+            grads = torch.ones(3, 16 * (1 + both), 2, device=DEV)
+            call([], s, both, grads)
+            dp.sync()
+            assert not grads.any()
+    for wrong in (torch.ones(3, 15, 2, device=DEV), torch.ones(16, 2, device=DEV), torch.ones(3, 16, 2, device=DEV).bfloat16()):
+        with pytest.raises((ValueError, TypeError)):
+            dp.relative_bias_grads([], s, False, wrong)
+    dp.sync()
